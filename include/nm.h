@@ -334,6 +334,92 @@ nm_status_t nm_maxpool2d(const float* x, int batch, int h, int w, int c, int kh,
                          int stride_w, int pad_h, int pad_w, float* y, void* cuda_stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Linear layers of language models in 8 bits.  The method prunes filter matrices; a linear layer is one (a pointwise
+ * convolution over tokens), and these entry points take it through serving arithmetic: activations as 8-bit integers
+ * with a scale for each token, column-wise N:M pruned weights as 8-bit integers with a scale for each output channel, exact
+ * sums.  Operators that make the activations (norm, gate, or none) hand them to nm_q8_linear as they are.
+ * Inference only.  Tensors may be strided: a row (token) is contiguous, `..._ld` is the distance of two rows in
+ * elements (at least the row's length; ignored for a single row).  No tokens (0) is a call that does nothing.
+ * ------------------------------------------------------------------------------------------- */
+
+/* Types of activations and outputs: fp32, bfloat16, fp16. */
+typedef enum { NM_F32 = 0, NM_BF16 = 1, NM_F16 = 2 } nm_dtype_t;
+
+/*
+ * Activations to 8-bit integers, a row (token) at a time:
+ *   a = max_j |p_j|,   q_j = the integer nearest to 127 p_j / a (ties to even),   scale = a / 127     (q_j scale stands for p_j)
+ * with
+ *   nm_q8_rows      p_j = x_j
+ *   nm_q8_silu_mul  p_j = up_j gate_j / (1 + exp(-gate_j))
+ *   nm_q8_rmsnorm   s_j = x_j + residual_j, rounded to `dtype` and written to `residual_out` (both NULL: s_j = x_j),
+ *                   p_j = s_j weight_j, and the norm's factor in the scale: scale = a / 127 / sqrt(mean_j s_j^2 + eps)
+ * q is the integer that exact arithmetic gives (up to double precision's own rounding), whatever kernel runs; sums are held in fp32 or more.  A row of zeros gives q = 0 and
+ * scale = 0.  A row that is not finite (a NaN or an infinity in s, in p, or a scale beyond fp32) gives q = 0 and scale = NaN: every
+ * product with that token is NaN then, and no other token's.
+ *   x, gate, up, residual, residual_out   device [tokens][h] of `dtype`, aligned to their elements (16-byte aligned rows are
+ *                   read 16 bytes at a time); residual_out may be residual or x themselves (same pointer and ld), else the
+ *                   outputs overlap no other tensor
+ *   weight          device [h] of `weight_dtype`: `dtype` or NM_F32
+ *   eps             1e-12 to 1
+ *   q               device int8 [tokens][q_ld], 16-byte aligned, q_ld a multiple of 16: the layout nm_q8_linear reads.
+ *                   Columns h to q_ld are left as they were
+ *   scale           device fp32 [tokens]
+ * h <= 65535.  Asynchronous on `cuda_stream`, which belongs to the current device like the tensors; allocates nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED (h), CUDA.
+ */
+nm_status_t nm_q8_rows(const void* x, long long x_ld, nm_dtype_t dtype, int tokens, int h, int8_t* q, long long q_ld,
+                       float* scale, void* cuda_stream);
+nm_status_t nm_q8_silu_mul(const void* gate, long long gate_ld, const void* up, long long up_ld, nm_dtype_t dtype, int tokens,
+                           int h, int8_t* q, long long q_ld, float* scale, void* cuda_stream);
+nm_status_t nm_q8_rmsnorm(const void* x, long long x_ld, const void* residual, long long residual_ld, void* residual_out,
+                          long long residual_out_ld, const void* weight, nm_dtype_t dtype, nm_dtype_t weight_dtype, int tokens,
+                          int h, float eps, int8_t* q, long long q_ld, float* scale, void* cuda_stream);
+
+/* Opaque handle of a linear layer's compressed 8-bit weights. */
+typedef struct nm_q8_weights nm_q8_weights_t;
+
+/*
+ * nm_prune's selection (column-wise N:M at tile level, Sec. 3.1, with its rules) on a dense fp32 filter matrix
+ * w_dense[c_out][k], and the retained weights of every row (output channel) as 8-bit integers:
+ *   scale[o] = max_j |w[o][idx_j]| / 127,   values[o][j] = the integer nearest to w[o][idx_j] / scale[o] (ties to even, from
+ *   the exact quotient).  A channel of zeros has scale 0, one with a NaN or an infinity scale NaN (its outputs are NaN).
+ * n_keep = m_group leaves the layer dense.  Allocates device memory and synchronises `cuda_stream`.
+ * Errors: as nm_prune; k, tile_t limits alike (k <= 65535, tile_t <= 256), c_out / tile_t at most 65535 tiles.
+ */
+nm_status_t nm_q8_prune(const float* w_dense, int c_out, int k, int n_keep, int m_group, int tile_t, void* cuda_stream,
+                        nm_q8_weights_t** out);
+
+/*
+ * A handle from an already compressed 8-bit layer (checkpoint path, inverse of nm_q8_weights_export):
+ *   values device int8 [c_out][kk], scales device fp32 [c_out], indices device uint16 [ceil(c_out / tile_t)][kk] as in
+ *   nm_weights_import (checked on the device: strictly ascending, below k, retained column j in group j / N), contiguous, of
+ *   the current device.  Synchronises `cuda_stream`.
+ */
+nm_status_t nm_q8_weights_import(const int8_t* values, const float* scales, const uint16_t* indices, int c_out, int k,
+                                 int n_keep, int m_group, int tile_t, void* cuda_stream, nm_q8_weights_t** out);
+/* Copies the canonical form to caller memory on `cuda_stream`; any pointer may be NULL. */
+nm_status_t nm_q8_weights_export(const nm_q8_weights_t* w, int8_t* values, float* scales, uint16_t* indices,
+                                 void* cuda_stream);
+nm_status_t nm_q8_weights_dims(const nm_q8_weights_t* w, int* c_out, int* k, int* kk, int* n_tiles, int* tile_t);
+/* As nm_weights_check and nm_weights_free. */
+nm_status_t nm_q8_weights_check(const nm_q8_weights_t* w, void* cuda_stream);
+nm_status_t nm_q8_weights_free(nm_q8_weights_t* w);
+
+/*
+ * y[t][o] = x_scale[t] scale[o] sum_j values[o][j] x[t][indices[o / tile_t][j]]  + bias[o]
+ * The sum is exact (32-bit integers hold 65535 products of 8-bit numbers), then converted and multiplied in fp32, by
+ * the token's scale first, the bias added, and rounded once to y's type.
+ *   x        device int8 [tokens][x_ld], 16-byte aligned, x_ld a multiple of 16 (not for a single token)
+ *   x_scale  device fp32 [tokens]          bias  device fp32 [c_out] or NULL
+ *   y        device [tokens][y_ld] of `y_dtype`, aligned to its elements; overlaps no input
+ * A token's output does not depend on the other tokens of the call or on their number.
+ * Asynchronous on `cuda_stream` (of the handle's device, which is the current one); allocates nothing.  Calls with one handle may overlap.
+ * Errors: INVALID_ARG, CUDA.
+ */
+nm_status_t nm_q8_linear(const nm_q8_weights_t* w, const int8_t* x, long long x_ld, const float* x_scale, int tokens,
+                         const float* bias, void* y, long long y_ld, nm_dtype_t y_dtype, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Auto-tuning (Sec. 3.3: profile kernel candidates on the target, keep the fastest)
  * ------------------------------------------------------------------------------------------- */
 

@@ -7,7 +7,9 @@
 // nm.py has loaded (NM_LIBRARY included) is the one that runs.
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/nm.h"
@@ -21,6 +23,10 @@ decltype(&nm_prune) p_prune = nullptr;
 decltype(&nm_weights_import) p_import = nullptr;
 decltype(&nm_weights_export) p_export = nullptr;
 decltype(&nm_weights_dims) p_dims = nullptr;
+decltype(&nm_q8_rows) p_q8_rows = nullptr;
+decltype(&nm_q8_silu_mul) p_q8_silu_mul = nullptr;
+decltype(&nm_q8_rmsnorm) p_q8_rmsnorm = nullptr;
+decltype(&nm_q8_linear) p_q8_linear = nullptr;
 
 void* current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 
@@ -275,6 +281,245 @@ PyObject* weights_export(PyObject*, PyObject* const* a, Py_ssize_t n)
     return Py_BuildValue("(NN)", vo, io);
 }
 
+// ---- 8-bit operators (tensors may be strided; they lie on one device, which is made the current one) ----
+
+bool dtype_of(at::ScalarType t, nm_dtype_t* out)
+{
+    if (t == at::kFloat) *out = NM_F32;
+    else if (t == at::kBFloat16) *out = NM_BF16;
+    else if (t == at::kHalf) *out = NM_F16;
+    else return false;
+    return true;
+}
+
+// A tensor [rows][cols] whose rows are contiguous, or NULL with a TypeError set; rows and cols of -1: any.
+const at::Tensor* matrix(PyObject* obj, const char* what, const char* type_name, bool type_ok(at::ScalarType), int64_t rows, int64_t cols,
+                         const at::Tensor* beside)
+{
+    if (THPVariable_Check(obj)) {
+        const at::Tensor& t = THPVariable_Unpack(obj);
+        if (t.is_cuda() && t.layout() == at::kStrided && type_ok(t.scalar_type()) && t.dim() == 2 && (t.size(1) < 2 || t.stride(1) == 1)) {
+            if ((rows >= 0 && t.size(0) != rows) || (cols >= 0 && t.size(1) != cols)) {
+                PyErr_Format(PyExc_TypeError, "%s must be [%lld, %lld] (got [%lld, %lld])", what, static_cast<long long>(rows >= 0 ? rows : t.size(0)),
+                             static_cast<long long>(cols >= 0 ? cols : t.size(1)), static_cast<long long>(t.size(0)), static_cast<long long>(t.size(1)));
+                return nullptr;
+            }
+            if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) {
+                PyErr_Format(PyExc_TypeError, "%s has too many rows or columns", what);
+                return nullptr;
+            }
+            if (beside && t.device() != beside->device()) {
+                PyErr_Format(PyExc_TypeError, "%s lies on another device", what);
+                return nullptr;
+            }
+            return &t;
+        }
+    }
+    PyErr_Format(PyExc_TypeError, "%s must be a two-dimensional %s CUDA tensor with contiguous rows", what, type_name);
+    return nullptr;
+}
+// A contiguous vector of `n` elements.
+const at::Tensor* vector(PyObject* obj, const char* what, const char* type_name, bool type_ok(at::ScalarType), int64_t n, const at::Tensor& beside)
+{
+    if (THPVariable_Check(obj)) {
+        const at::Tensor& t = THPVariable_Unpack(obj);
+        if (t.is_cuda() && t.layout() == at::kStrided && type_ok(t.scalar_type()) && t.dim() == 1 && t.is_contiguous() && t.size(0) == n &&
+            t.device() == beside.device())
+            return &t;
+    }
+    PyErr_Format(PyExc_TypeError, "%s must be a contiguous %s CUDA tensor of %lld elements on the same device", what, type_name, static_cast<long long>(n));
+    return nullptr;
+}
+bool is_float_type(at::ScalarType t)
+{
+    nm_dtype_t d;
+    return dtype_of(t, &d);
+}
+bool is_f32(at::ScalarType t) { return t == at::kFloat; }
+bool is_s8(at::ScalarType t) { return t == at::kChar; }
+const char* const kFloats = "float32, bfloat16 or float16";
+
+// q and scale of `x`'s rows: those given, or new ones (rows of q a multiple of 16 bytes apart).
+bool quantised_out(const at::Tensor& x, PyObject* q_obj, PyObject* scale_obj, at::Tensor* q, at::Tensor* scale)
+{
+    const int64_t tokens = x.size(0), h = x.size(1);
+    if (q_obj == Py_None) {
+        *q = at::empty_strided({tokens, h}, {(h + 15) / 16 * 16, 1}, x.options().dtype(at::kChar));
+    } else {
+        const at::Tensor* t = matrix(q_obj, "q", "int8", is_s8, tokens, h, &x);
+        if (!t) return false;
+        *q = *t;
+    }
+    if (scale_obj == Py_None) {
+        *scale = at::empty({tokens}, x.options().dtype(at::kFloat));
+    } else {
+        const at::Tensor* t = vector(scale_obj, "scale", "float32", is_f32, tokens, x);
+        if (!t) return false;
+        *scale = *t;
+    }
+    return true;
+}
+
+PyObject* tensors(at::Tensor a, at::Tensor b, at::Tensor c)
+{
+    PyObject* out = PyTuple_New(c.defined() ? 3 : 2);
+    if (!out) return nullptr;
+    at::Tensor all[3] = {std::move(a), std::move(b), std::move(c)};
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(out); ++i) {
+        PyObject* o = THPVariable_Wrap(std::move(all[i]));
+        if (!o) {
+            Py_DECREF(out);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(out, i, o);
+    }
+    return out;
+}
+
+// q8_rows(x, q, scale) and q8_silu_mul(gate, up, q, scale) -> (q, scale), or the status as an int
+PyObject* q8_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 3 && n != 4) {
+        PyErr_SetString(PyExc_TypeError, "q8_rows takes 3 or 4 arguments");
+        return nullptr;
+    }
+    const bool gated = n == 4;
+    const at::Tensor* x = matrix(a[0], gated ? "gate" : "x", kFloats, is_float_type, -1, -1, nullptr);
+    if (!x) return nullptr;
+    const at::Tensor* up = nullptr;
+    if (gated) {
+        up = matrix(a[1], "up", kFloats, is_float_type, x->size(0), x->size(1), x);
+        if (!up) return nullptr;
+        if (up->scalar_type() != x->scalar_type()) {
+            PyErr_SetString(PyExc_TypeError, "up must have gate's type");
+            return nullptr;
+        }
+    }
+    const c10::cuda::CUDAGuard guard(x->device());
+    at::Tensor q, scale;
+    if (!quantised_out(*x, a[n - 2], a[n - 1], &q, &scale)) return nullptr;
+    nm_dtype_t type = NM_F32;
+    dtype_of(x->scalar_type(), &type);
+    const int tokens = static_cast<int>(x->size(0)), h = static_cast<int>(x->size(1));
+    const void* xp = x->const_data_ptr();
+    const void* up_p = up ? up->const_data_ptr() : nullptr;
+    const long long x_ld = x->stride(0), up_ld = up ? up->stride(0) : 0, q_ld = q.stride(0);
+    auto* qp = static_cast<int8_t*>(q.mutable_data_ptr());
+    float* sp = scale.mutable_data_ptr<float>();
+    void* st = current_stream();
+    nm_status_t s;
+    Py_BEGIN_ALLOW_THREADS
+    s = gated ? p_q8_silu_mul(xp, x_ld, up_p, up_ld, type, tokens, h, qp, q_ld, sp, st) : p_q8_rows(xp, x_ld, type, tokens, h, qp, q_ld, sp, st);
+    Py_END_ALLOW_THREADS
+    if (s != NM_OK) return PyLong_FromLong(s);
+    return tensors(std::move(q), std::move(scale), at::Tensor());
+}
+
+// q8_rmsnorm(x, weight, eps, residual, residual_out, q, scale) -> (q, scale) or (q, scale, residual_out), or the status as an int
+PyObject* q8_rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 7) {
+        PyErr_SetString(PyExc_TypeError, "q8_rmsnorm takes 7 arguments");
+        return nullptr;
+    }
+    const at::Tensor* x = matrix(a[0], "x", kFloats, is_float_type, -1, -1, nullptr);
+    if (!x) return nullptr;
+    const at::Tensor* weight = vector(a[1], "weight", kFloats, is_float_type, x->size(1), *x);
+    if (!weight) return nullptr;
+    const double eps = PyFloat_AsDouble(a[2]);
+    if (PyErr_Occurred()) return nullptr;
+    const c10::cuda::CUDAGuard guard(x->device());
+    const at::Tensor* residual = nullptr;
+    at::Tensor out;
+    if (a[3] != Py_None) {
+        residual = matrix(a[3], "residual", kFloats, is_float_type, x->size(0), x->size(1), x);
+        if (!residual) return nullptr;
+        if (a[4] == Py_None) {
+            out = at::empty({x->size(0), x->size(1)}, x->options());
+        } else {
+            const at::Tensor* t = matrix(a[4], "residual_out", kFloats, is_float_type, x->size(0), x->size(1), x);
+            if (!t) return nullptr;
+            out = *t;
+        }
+        if (residual->scalar_type() != x->scalar_type() || out.scalar_type() != x->scalar_type()) {
+            PyErr_SetString(PyExc_TypeError, "residual and residual_out must have x's type");
+            return nullptr;
+        }
+    } else if (a[4] != Py_None) {
+        PyErr_SetString(PyExc_TypeError, "residual_out without a residual");
+        return nullptr;
+    }
+    at::Tensor q, scale;
+    if (!quantised_out(*x, a[5], a[6], &q, &scale)) return nullptr;
+    nm_dtype_t type = NM_F32, weight_type = NM_F32;
+    dtype_of(x->scalar_type(), &type);
+    dtype_of(weight->scalar_type(), &weight_type);
+    const int tokens = static_cast<int>(x->size(0)), h = static_cast<int>(x->size(1));
+    const void *xp = x->const_data_ptr(), *wp = weight->const_data_ptr(), *rp = residual ? residual->const_data_ptr() : nullptr;
+    void* op = residual ? out.mutable_data_ptr() : nullptr;
+    const long long x_ld = x->stride(0), r_ld = residual ? residual->stride(0) : 0, o_ld = residual ? out.stride(0) : 0, q_ld = q.stride(0);
+    auto* qp = static_cast<int8_t*>(q.mutable_data_ptr());
+    float* sp = scale.mutable_data_ptr<float>();
+    void* st = current_stream();
+    nm_status_t s;
+    Py_BEGIN_ALLOW_THREADS
+    s = p_q8_rmsnorm(xp, x_ld, rp, r_ld, op, o_ld, wp, type, weight_type, tokens, h, static_cast<float>(eps), qp, q_ld, sp, st);
+    Py_END_ALLOW_THREADS
+    if (s != NM_OK) return PyLong_FromLong(s);
+    return tensors(std::move(q), std::move(scale), std::move(out));
+}
+
+// q8_linear(handle, c_out, k, xq, x_scale, bias, out_dtype, y) -> y, or the status as an int
+PyObject* q8_linear(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 8) {
+        PyErr_SetString(PyExc_TypeError, "q8_linear takes 8 arguments");
+        return nullptr;
+    }
+    const auto* w = static_cast<const nm_q8_weights_t*>(PyLong_AsVoidPtr(a[0]));
+    int dims[2];
+    if (PyErr_Occurred() || !ints_of(a + 1, 2, dims)) return nullptr;
+    const at::Tensor* x = matrix(a[3], "xq", "int8", is_s8, -1, dims[1], nullptr);
+    if (!x) return nullptr;
+    const at::Tensor* x_scale = vector(a[4], "x_scale", "float32", is_f32, x->size(0), *x);
+    if (!x_scale) return nullptr;
+    const at::Tensor* bias = nullptr;
+    if (a[5] != Py_None) {
+        bias = vector(a[5], "bias", "float32", is_f32, dims[0], *x);
+        if (!bias) return nullptr;
+    }
+    const c10::cuda::CUDAGuard guard(x->device());
+    at::Tensor made;
+    const at::Tensor* y;
+    if (a[7] == Py_None) {
+        if (!THPDtype_Check(a[6]) || !is_float_type(reinterpret_cast<THPDtype*>(a[6])->scalar_type)) {
+            PyErr_Format(PyExc_TypeError, "out_dtype must be %s", kFloats);
+            return nullptr;
+        }
+        made = at::empty({x->size(0), dims[0]}, x->options().dtype(reinterpret_cast<THPDtype*>(a[6])->scalar_type));
+        y = &made;
+    } else {
+        y = matrix(a[7], "y", kFloats, is_float_type, x->size(0), dims[0], x);
+        if (!y) return nullptr;
+    }
+    nm_dtype_t type = NM_F32;
+    dtype_of(y->scalar_type(), &type);
+    const auto* xp = static_cast<const int8_t*>(x->const_data_ptr());
+    const float *sp = x_scale->const_data_ptr<float>(), *bp = bias ? bias->const_data_ptr<float>() : nullptr;
+    void* yp = y->mutable_data_ptr();
+    const int tokens = static_cast<int>(x->size(0));
+    const long long x_ld = x->stride(0), y_ld = y->stride(0);
+    void* st = current_stream();
+    nm_status_t s;
+    Py_BEGIN_ALLOW_THREADS
+    s = p_q8_linear(w, xp, x_ld, sp, tokens, bp, yp, y_ld, type, st);
+    Py_END_ALLOW_THREADS
+    if (s != NM_OK) return PyLong_FromLong(s);
+    if (a[7] == Py_None) return THPVariable_Wrap(std::move(made));
+    Py_INCREF(a[7]);
+    return a[7];
+}
+
 PyObject* stream_ptr(PyObject*, PyObject* const*, Py_ssize_t n)
 {
     if (n != 0) {
@@ -286,8 +531,8 @@ PyObject* stream_ptr(PyObject*, PyObject* const*, Py_ssize_t n)
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 7) {
-        PyErr_SetString(PyExc_TypeError, "bind takes 7 addresses");
+    if (n != 11) {
+        PyErr_SetString(PyExc_TypeError, "bind takes 11 addresses");
         return nullptr;
     }
     p_conv2d = reinterpret_cast<decltype(p_conv2d)>(PyLong_AsVoidPtr(a[0]));
@@ -297,6 +542,10 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
     p_import = reinterpret_cast<decltype(p_import)>(PyLong_AsVoidPtr(a[4]));
     p_export = reinterpret_cast<decltype(p_export)>(PyLong_AsVoidPtr(a[5]));
     p_dims = reinterpret_cast<decltype(p_dims)>(PyLong_AsVoidPtr(a[6]));
+    p_q8_rows = reinterpret_cast<decltype(p_q8_rows)>(PyLong_AsVoidPtr(a[7]));
+    p_q8_silu_mul = reinterpret_cast<decltype(p_q8_silu_mul)>(PyLong_AsVoidPtr(a[8]));
+    p_q8_rmsnorm = reinterpret_cast<decltype(p_q8_rmsnorm)>(PyLong_AsVoidPtr(a[9]));
+    p_q8_linear = reinterpret_cast<decltype(p_q8_linear)>(PyLong_AsVoidPtr(a[10]));
     if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NONE;
 }
@@ -327,6 +576,9 @@ PyMethodDef methods[] = {
     {"prune", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<prune>)), METH_FASTCALL, nullptr},
     {"weights_import", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<weights_import>)), METH_FASTCALL, nullptr},
     {"weights_export", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<weights_export>)), METH_FASTCALL, nullptr},
+    {"q8_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<q8_rows>)), METH_FASTCALL, nullptr},
+    {"q8_rmsnorm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<q8_rmsnorm>)), METH_FASTCALL, nullptr},
+    {"q8_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<q8_linear>)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
     {"stream_ptr", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<stream_ptr>)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -15,6 +15,7 @@
 
 #include "nm_internal.h"
 #include "nm_ptx.cuh"
+#include "nm_q8.h"
 
 namespace {
 
@@ -71,8 +72,8 @@ __global__ void k_mass(const double* __restrict__ score, const uint8_t* __restri
     }
 }
 
-__global__ void k_compact(const uint8_t* __restrict__ keep, int k, int kk, int n_keep, int m_group,
-                          uint16_t* __restrict__ indices)
+__global__ void k_compact(const uint8_t* __restrict__ keep, int k, int kk, int kk_ld, int n_keep, int m_group,
+                          uint16_t* __restrict__ indices)   // (kk_ld: pitch of a row of indices)
 {
     const int col = blockIdx.x * blockDim.x + threadIdx.x;
     const int r = blockIdx.y;
@@ -85,7 +86,7 @@ __global__ void k_compact(const uint8_t* __restrict__ keep, int k, int kk, int n
     // a group never holds more than N kept columns (the order of the scores is total); the bound
     // makes sure that no input whatsoever can place a column outside its group's slots
     if (pos >= min(kk, (g + 1) * n_keep)) return;
-    indices[static_cast<size_t>(r) * kk + pos] = static_cast<uint16_t>(col);
+    indices[static_cast<size_t>(r) * kk_ld + pos] = static_cast<uint16_t>(col);
 }
 
 // Groups wider than a block of k_compress.
@@ -100,12 +101,9 @@ nm_status_t prune_wide(const float* w_dense, nm_weights* h, cudaStream_t st, dou
     if (!scratch) return fail(NM_ERR_ALLOC, "nm_prune: cannot allocate %zu bytes of scratch", cells * 9);
     double* score = reinterpret_cast<double*>(scratch);
     uint8_t* keep = scratch + cells * sizeof(double);
-    const dim3 blk(128), grid((h->k + 127) / 128, h->n_tiles);
-    k_score<<<grid, blk, 0, st>>>(w_dense, h->c_out, h->k, h->tile_t, score);
-    k_select<<<grid, blk, 0, st>>>(score, h->k, h->n_keep, h->m_group, keep);
-    k_compact<<<grid, blk, 0, st>>>(keep, h->k, h->kk, h->n_keep, h->m_group, h->indices);
+    select_columns(w_dense, h->c_out, h->k, h->kk, h->kk, h->n_keep, h->m_group, h->tile_t, score, keep, h->indices, st);
     k_mass<<<static_cast<unsigned>(std::min<size_t>((cells + 255) / 256, 1024)), 256, 0, st>>>(score, keep, cells, h->mass);
-    count_launch(4);
+    count_launch(1);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) st_out = fail(NM_ERR_CUDA, "pruning kernels: %s", cudaGetErrorString(e));
     if (st_out == NM_OK) st_out = build_layouts(h, w_dense, h->indices, false, st);
@@ -117,6 +115,16 @@ nm_status_t prune_wide(const float* w_dense, nm_weights* h, cudaStream_t st, dou
 }  // namespace
 
 namespace nmhost {
+
+void select_columns(const float* w_dense, int c_out, int k, int kk, int kk_ld, int n_keep, int m_group, int tile_t, double* score,
+                    uint8_t* keep, uint16_t* indices, cudaStream_t st)
+{
+    const dim3 blk(128), grid((k + 127) / 128, (c_out + tile_t - 1) / tile_t);
+    k_score<<<grid, blk, 0, st>>>(w_dense, c_out, k, tile_t, score);
+    k_select<<<grid, blk, 0, st>>>(score, k, n_keep, m_group, keep);
+    k_compact<<<grid, blk, 0, st>>>(keep, k, kk, kk_ld, n_keep, m_group, indices);
+    count_launch(3);
+}
 
 nm_status_t prune_on_device(const float* w_dense, nm_weights* h, cudaStream_t st)
 {

@@ -436,6 +436,25 @@ __device__ __forceinline__ void umma_tf32_ss(uint32_t d_tmem, uint64_t adesc, ui
         "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// Instruction descriptor: signed 8-bit x signed 8-bit -> 32-bit integers, both operands K-major, shape m x n (x 32).
+__host__ __device__ constexpr uint32_t umma_idesc_s8(int m, int n)
+{
+    return (2u << 4)                                  // D: 32-bit integers
+           | (1u << 7) | (1u << 10)                   // A, B: signed 8-bit
+           | (static_cast<uint32_t>(n >> 3) << 17)    // N / 8
+           | (static_cast<uint32_t>(m >> 4) << 24);   // M / 16
+}
+__device__ __forceinline__ void umma_s8_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t"
+        "}\n" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 // Arrives on `bar` once every MMA issued so far by this thread has finished.
 __device__ __forceinline__ void umma_commit(uint32_t bar)
 {

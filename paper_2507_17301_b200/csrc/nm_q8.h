@@ -1,0 +1,69 @@
+// Declarations shared by the translation units of the 8-bit operators.
+#pragma once
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "nm_internal.h"
+
+constexpr uint32_t NM_Q8_MAGIC = 0x4E4D5138u;   // "NMQ8"
+
+// Compressed 8-bit weights of one linear layer.
+struct nm_q8_weights {
+    uint32_t magic;
+    int device;
+    uint8_t* block;        // the handle's device memory: one allocation that every array below lies in
+    size_t block_bytes;
+    int c_out, k, kk, n_keep, m_group, tile_t, n_tiles;
+    int kk_ld;             // row pitch of `values` and `indices`: kk rounded up to a multiple of 64 (zeros in between)
+    int k_blocks, rows;    // of `expanded`: ceil(k / 128) blocks, c_out rounded up to a multiple of 256
+    int8_t* values;        // [c_out][kk_ld]
+    float* scales;         // [c_out]
+    uint16_t* indices;     // [n_tiles][kk_ld]
+    int8_t* expanded;      // [k_blocks][rows][128]: pruned columns are zeros; a row's eight 16-byte pieces stand in the order of the
+                           // tensor core's 128-byte swizzle (piece i of row r at i ^ (r & 7))
+    int* status;           // device int[4], as in nm_weights
+};
+
+// One call of a row operator (strides in elements).
+struct Q8Rows {
+    const void* x;         // rmsnorm, rows: input; silu_mul: gate
+    long long x_ld;
+    const void* r;         // rmsnorm: residual or NULL; silu_mul: up
+    long long r_ld;
+    void* s;               // rmsnorm with a residual: x + r
+    long long s_ld;
+    const void* weight;    // rmsnorm
+    int tokens, h;
+    float eps;
+    int8_t* q;
+    long long q_ld;
+    float* scale;
+};
+enum Q8RowOp { Q8_RMSNORM = 0, Q8_SILU_MUL = 1, Q8_ROWS = 2 };
+
+// One call of the product.
+struct Q8Linear {
+    const nm_q8_weights* w;
+    const int8_t* x;       // [tokens][x_ld]
+    long long x_ld;
+    const float* x_scale;
+    const float* bias;     // or NULL
+    void* y;               // [tokens][y_ld]
+    long long y_ld;
+    int tokens;
+    nm_dtype_t y_type;
+};
+
+namespace nmhost {
+// nm_q8_rows_*.cu, one per type of the activations
+nm_status_t launch_q8_rows_f32(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
+nm_status_t launch_q8_rows_bf16(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
+nm_status_t launch_q8_rows_f16(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
+
+// nm_q8_gemm.cu
+nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st);
+
+// nm_prune.cu: retained columns of every tile by their L1 norms; `score` and `keep`: scratch of n_tiles * k entries each
+void select_columns(const float* w_dense, int c_out, int k, int kk, int kk_ld, int n_keep, int m_group, int tile_t, double* score,
+                    uint8_t* keep, uint16_t* indices, cudaStream_t st);
+}  // namespace nmhost

@@ -1,0 +1,265 @@
+// Product of 8-bit activations with column-wise N:M pruned 8-bit weights on the tensor core (kind::i8, exact 32-bit sums).
+//
+//   D[channel][token] = sum over 128-column blocks of  W[128 channels x 128] * X[BN tokens x 128]^T
+//
+// Weights are the M side (128 channels a tile), tokens the N side (16 to 256), so that a few tokens fill an instruction as well as
+// many.  Pruned columns are zeros of the expanded weights: the 16 KB of a tile and block lie in memory as the swizzled
+// shared-memory image, one bulk copy; activations come by TMA, zeros past the last column and token.
+// Where there are far fewer tiles than SMs the reduction axis is split over the 2, 4 or 8 CTAs of a cluster: each sends the runs of tokens
+// that another finishes as one bulk copy into that CTA's shared memory.  Sums are integers: the result does not depend on the split.
+//
+//   producer (1 thread), MMA issuer (1 thread), epilogue (4 warps, a lane per channel): y = (sum * x_scale) * w_scale + bias
+#include <algorithm>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "nm_ptx.cuh"
+#include "nm_q8.h"
+#include "nm_tmap.cuh"
+
+namespace {
+
+using namespace nmk;
+
+constexpr int THREADS = 192;   // warps: 0 producer, 1 MMA issuer and tensor memory, 2-5 epilogue
+constexpr int NSTAGE_MAX = 8;
+constexpr int A_BYTES = 128 * 128;
+
+struct GemmArgs {
+    const int8_t* expanded;
+    const float* w_scale;
+    const float* x_scale;
+    const float* bias;
+    void* y;
+    long long y_ld;
+    int* status;
+    int tokens, c_out, rows, k_blocks;
+    int c_tiles;
+    int bn;
+    int ks;       // CTAs of a cluster = ranges of the reduction axis
+    int stages, stage_bytes;
+};
+
+template <typename T>
+__device__ __forceinline__ void put(void* y, size_t at, float v);
+template <>
+__device__ __forceinline__ void put<float>(void* y, size_t at, float v) { static_cast<float*>(y)[at] = v; }
+template <>
+__device__ __forceinline__ void put<__nv_bfloat16>(void* y, size_t at, float v) { static_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ void put<__half>(void* y, size_t at, float v) { static_cast<__half*>(y)[at] = __float2half_rn(v); }
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS, 1) k_q8_gemm(const GemmArgs g, const __grid_constant__ CUtensorMap tm_x)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t s_full[NSTAGE_MAX], s_free[NSTAGE_MAX], s_acc, s_recv;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    __shared__ float s_scale[256];   // of the tile's tokens
+
+    const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
+    const uint32_t rank = g.ks > 1 ? cluster_ctarank() : 0u;
+    const int item = static_cast<int>(blockIdx.x) / g.ks;
+    const int c0 = item % g.c_tiles * 128;                 // consecutive items share their tokens
+    const int t0 = item / g.c_tiles * g.bn;
+    const int kb0 = static_cast<int>(static_cast<long long>(g.k_blocks) * rank / g.ks), kb1 = static_cast<int>(static_cast<long long>(g.k_blocks) * (rank + 1) / g.ks);
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t recv = ring + g.stages * g.stage_bytes;   // [ks][bn / ks tokens][128 channels] (ks > 1)
+    volatile int* abort_flag = &s_abort;
+
+    if (warp == 1) tmem_alloc(smem_u32(&s_tmem), g.bn < 32 ? 32 : g.bn);
+    if (tid == 0) {
+        for (int i = 0; i < NSTAGE_MAX; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_free[i]), 1);
+        }
+        mbar_init(smem_u32(&s_acc), 1);
+        mbar_init(smem_u32(&s_recv), 1);
+        mbar_fence_init();
+        if (g.ks > 1) mbar_arrive_expect_tx(smem_u32(&s_recv), static_cast<uint32_t>(g.bn) * 512u);
+        s_abort = 0;
+        tma_prefetch_desc(&tm_x);
+    }
+    tc_fence_before();
+    if (g.ks > 1) cluster_sync_all();   // the other CTAs' barriers are initialised before anything is sent to them
+    else __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    pdl_launch_dependents();            // (after the allocation: what starts now cannot take tensor memory that this launch still wants)
+
+    if (warp == 0) {
+        if (elect_one()) {
+            const int8_t* src = g.expanded + (static_cast<size_t>(kb0) * g.rows + c0) * 128;
+            const uint32_t tx = static_cast<uint32_t>(A_BYTES + g.bn * 128);
+            RingPos rp;
+            int issued = 0;
+            bool after = false;   // the kernel before has ended
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (rp.wrapped && !mbar_wait_lone(smem_u32(&s_free[rp.s]), rp.parity ^ 1u)) { *abort_flag = 1; break; }
+                const uint32_t at = ring + rp.s * g.stage_bytes, bar = smem_u32(&s_full[rp.s]);
+                mbar_arrive_expect_tx(bar, tx);
+                bulk_load_1d(at, src, A_BYTES, bar);   // weights: no kernel of the stream writes them
+                if (!after) pdl_wait();
+                after = true;
+                tma_load_2d(at + A_BYTES, &tm_x, bar, kb * 128, t0);
+                src += static_cast<size_t>(g.rows) * 128;
+                rp.advance(g.stages);
+                ++issued;
+            }
+            if (!after) pdl_wait();
+            if (*abort_flag != 0) {
+                // let the loads in flight land
+                for (int back = 0; back < g.stages && back < issued; ++back) {
+                    if (rp.s == 0) { rp.s = g.stages; rp.parity ^= 1u; }
+                    --rp.s;
+                    (void)mbar_wait(smem_u32(&s_full[rp.s]), rp.parity);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            const uint32_t idesc = umma_idesc_s8(128, g.bn);
+            RingPos rp;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!mbar_wait_lone(smem_u32(&s_full[rp.s]), rp.parity)) { *abort_flag = 2; break; }
+                tc_fence_after();
+                const uint32_t at = ring + rp.s * g.stage_bytes;
+                const uint64_t adesc = umma_desc_k_sw128(at, 1024), bdesc = umma_desc_k_sw128(at + A_BYTES, 1024);
+#pragma unroll
+                for (int kq = 0; kq < 4; ++kq) umma_s8_ss(tmem, adesc + 2 * kq, bdesc + 2 * kq, idesc, (kb > kb0 || kq > 0) ? 1u : 0u);
+                umma_commit(smem_u32(&s_free[rp.s]));
+                rp.advance(g.stages);
+            }
+            umma_commit(smem_u32(&s_acc));
+        }
+    } else {
+        pdl_wait();
+        const int e = tid - 64;   // 0 to 127
+        for (int i = e; i < g.bn; i += 128) s_scale[i] = t0 + i < g.tokens ? __ldg(g.x_scale + t0 + i) : 0.f;
+        const int q = warp & 3;
+        const int row = q * 32 + lane, ch = c0 + row;
+        const float ws = ch < g.c_out ? __ldg(g.w_scale + ch) : 0.f;
+        const float bias = g.bias && ch < g.c_out ? __ldg(g.bias + ch) : 0.f;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const bool ok = mbar_wait(smem_u32(&s_acc), 0);
+        if (!ok) *abort_flag = 3;
+        tc_fence_after();
+        const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16);
+        if (g.ks == 1) {
+            for (int b = 0; b < g.bn; b += 16) {
+                uint32_t v[16];
+                tmem_ld16(mine + b, v);
+                tmem_ld_wait();
+                if (ok && ch < g.c_out) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t0 + b + i < g.tokens)
+                            put<T>(g.y, static_cast<size_t>(t0 + b + i) * g.y_ld + ch, fmaf(static_cast<float>(static_cast<int>(v[i])) * s_scale[b + i], ws, bias));
+                }
+            }
+        } else {
+            // partial sums by token into the ring, whose loads have all been used; then each CTA's run of tokens to that CTA
+            for (int b = 0; b < g.bn; b += 16) {
+                uint32_t v[16];
+                tmem_ld16(mine + b, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(ring + static_cast<uint32_t>((b + i) * 128 + row) * 4u), "r"(v[i]) : "memory");
+            }
+            fence_proxy_async();
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            const int run = g.bn / g.ks;
+            if (e == 0) {
+                for (int d = 0; d < g.ks; ++d)
+                    bulk_copy_cluster(mapa_shared(recv + rank * run * 512u, d), ring + static_cast<uint32_t>(d * run) * 512u, static_cast<uint32_t>(run) * 512u,
+                                      mapa_shared(smem_u32(&s_recv), d));
+            }
+            if (!mbar_wait_cluster(smem_u32(&s_recv), 0)) *abort_flag = 4;
+            else if (ch < g.c_out) {
+                for (int i = 0; i < run; ++i) {
+                    int sum = 0;
+                    for (int s = 0; s < g.ks; ++s) {
+                        int v;
+                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(recv + static_cast<uint32_t>((s * run + i) * 128 + row) * 4u) : "memory");
+                        sum += v;
+                    }
+                    const int at = static_cast<int>(rank) * run + i;
+                    if (t0 + at < g.tokens)
+                        put<T>(g.y, static_cast<size_t>(t0 + at) * g.y_ld + ch, fmaf(static_cast<float>(sum) * s_scale[at], ws, bias));
+                }
+            }
+        }
+    }
+
+    tc_fence_before();
+    if (g.ks > 1) cluster_sync_all();   // nobody leaves while its shared memory is read or written by another CTA
+    else __syncthreads();
+    if (tid == 0 && s_abort != 0) {
+        atomicExch(g.status + 0, static_cast<int>(NM_ERR_TIMEOUT));
+        atomicExch(g.status + 1, 200 + s_abort);
+        atomicExch(g.status + 2, static_cast<int>(blockIdx.x));
+    }
+    if (warp == 1) tmem_dealloc(tmem, g.bn < 32 ? 32 : g.bn);
+}
+
+}  // namespace
+
+namespace nmhost {
+
+nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
+{
+    const nm_q8_weights* w = p.w;
+    GemmArgs g = {};
+    g.expanded = w->expanded; g.w_scale = w->scales; g.x_scale = p.x_scale; g.bias = p.bias; g.y = p.y; g.y_ld = p.y_ld; g.status = w->status;
+    g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows; g.k_blocks = w->k_blocks;
+    g.c_tiles = (w->c_out + 127) / 128;
+    g.bn = 16;
+    while (g.bn < 256 && g.bn < p.tokens) g.bn *= 2;
+    // far fewer tiles than SMs: narrower ones (a split has to hold a tile's partial sums beside the ring)
+    while (g.bn == 256 && 2ll * g.c_tiles * ((p.tokens + 255) / 256) <= sm_count()) g.bn = 128;
+    const long long items = static_cast<long long>(g.c_tiles) * ((p.tokens + g.bn - 1) / g.bn);
+    if (items > (1ll << 27)) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: too many tiles");
+    g.ks = 1;
+    while (g.bn <= 128 && g.ks < 8 && items * g.ks * 2 <= sm_count() && g.k_blocks >= g.ks * 4) g.ks *= 2;
+    g.stage_bytes = A_BYTES + g.bn * 128;
+    const int budget = 227 * 1024 - 1024 - 2048 - (g.ks > 1 ? g.bn * 512 : 0);
+    g.stages = std::min(NSTAGE_MAX, budget / g.stage_bytes);
+    // (a split's partial sums, at most 64 KB, go through the ring, which has at least 144 KB then)
+    CUtensorMap tm;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(w->k), static_cast<cuuint64_t>(p.tokens)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.x_ld)};
+    const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(g.bn)}, es[2] = {1, 1};
+    if (!nmtm::available() ||
+        nmtm::encoders().tiled(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(p.x), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return fail(NM_ERR_CUDA, "nm_q8_linear: tensor-map encoding failed");
+    size_t smem = 1024 + static_cast<size_t>(g.stages) * g.stage_bytes + (g.ks > 1 ? g.bn * 512 : 0);
+    if (smem < NM_EXCLUSIVE_SMEM) smem = NM_EXCLUSIVE_SMEM;   // alone on its SM: CTAs of a cluster wait for each other while they hold tensor memory
+    void (*kernel)(GemmArgs, CUtensorMap) = p.y_type == NM_F32 ? k_q8_gemm<float> : p.y_type == NM_BF16 ? k_q8_gemm<__nv_bfloat16> : k_q8_gemm<__half>;
+    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
+    if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear: cudaFuncSetAttribute: %s", cudaGetErrorString(e));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(items * g.ks));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(g.ks);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, g, tm);
+    count_launch(1);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear launch: %s", cudaGetErrorString(e));
+    return NM_OK;
+}
+
+}  // namespace nmhost

@@ -87,6 +87,20 @@ def _load():
     lib.nm_plan_cache_lookup.restype = ctypes.c_int
     lib.nm_memory_trim.argtypes = []
     lib.nm_memory_trim.restype = ctypes.c_int
+    ll, f = ctypes.c_longlong, ctypes.c_float
+    lib.nm_q8_rows.argtypes = [vp, ll, i, i, i, vp, ll, vp, vp]
+    lib.nm_q8_silu_mul.argtypes = [vp, ll, vp, ll, i, i, i, vp, ll, vp, vp]
+    lib.nm_q8_rmsnorm.argtypes = [vp, ll, vp, ll, vp, ll, vp, i, i, i, i, f, vp, ll, vp, vp]
+    lib.nm_q8_prune.argtypes = [vp, i, i, i, i, i, vp, ctypes.POINTER(vp)]
+    lib.nm_q8_weights_import.argtypes = [vp, vp, vp, i, i, i, i, i, vp, ctypes.POINTER(vp)]
+    lib.nm_q8_weights_export.argtypes = [vp, vp, vp, vp, vp]
+    lib.nm_q8_weights_dims.argtypes = [vp, ip, ip, ip, ip, ip]
+    lib.nm_q8_weights_check.argtypes = [vp, vp]
+    lib.nm_q8_weights_free.argtypes = [vp]
+    lib.nm_q8_linear.argtypes = [vp, vp, ll, vp, i, vp, vp, ll, i, vp]
+    for name in ("rows", "silu_mul", "rmsnorm", "prune", "weights_import", "weights_export", "weights_dims", "weights_check",
+                 "weights_free", "linear"):
+        getattr(lib, "nm_q8_" + name).restype = ctypes.c_int
     lib.nm_status_string.argtypes = [ctypes.c_int]
     lib.nm_status_string.restype = ctypes.c_char_p
     lib.nm_last_error.argtypes = []
@@ -104,10 +118,13 @@ except ImportError as e:
     raise ImportError("the CPython extension _nm_binding is not built; run `python -m paper_2507_17301_b200.build` "
                       f"(there is no fallback path without it): {e}") from e
 _nm_binding.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-    _lib.nm_conv2d, _lib.nm_conv2d_res, _lib.nm_maxpool2d, _lib.nm_prune, _lib.nm_weights_import, _lib.nm_weights_export, _lib.nm_weights_dims)))
+    _lib.nm_conv2d, _lib.nm_conv2d_res, _lib.nm_maxpool2d, _lib.nm_prune, _lib.nm_weights_import, _lib.nm_weights_export, _lib.nm_weights_dims,
+    _lib.nm_q8_rows, _lib.nm_q8_silu_mul, _lib.nm_q8_rmsnorm, _lib.nm_q8_linear)))
 
 EXPORTS = ("nm_memory_trim", "nm_plan_key", "nm_plan_cache_store", "nm_plan_cache_lookup", "nm_selftest_wait_expiry", "nm_maxpool2d", "nm_weights_retained_l1", "nm_conv2d_res", "nm_plan_scratch_bytes", "nm_weights_reserve", "nm_prune", "nm_prune_noalloc", "nm_weights_dims", "nm_weights_export", "nm_weights_import", "nm_weights_check",
            "nm_weights_free", "nm_conv2d", "nm_conv2d_host", "nm_autotune", "nm_autotune_tile",
+           "nm_q8_rows", "nm_q8_silu_mul", "nm_q8_rmsnorm", "nm_q8_prune", "nm_q8_weights_import", "nm_q8_weights_export",
+           "nm_q8_weights_dims", "nm_q8_weights_check", "nm_q8_weights_free", "nm_q8_linear",
            "nm_status_string", "nm_last_error", "nm_launch_count")
 
 
@@ -364,3 +381,116 @@ def nm_autotune_tile(w_dense: torch.Tensor, n_keep: int, m_group: int, tile_cand
                                  int(bool(relu)), _dev_f32(y_scratch, "y_scratch"), _stream(), ctypes.byref(tile),
                                  ctypes.byref(plan), ctypes.byref(ms)))
     return int(tile.value), plan, float(ms.value)
+
+
+# ---- linear layers of language models in 8 bits -------------------------------------------------------------------
+
+
+class Q8Weights:
+    """Owner of one ``nm_q8_weights_t*`` handle (freed with the object)."""
+
+    def __init__(self, handle: int):
+        self._h = ctypes.c_void_p(handle)
+        self._addr = handle or 0
+        out = [ctypes.c_int() for _ in range(5)]
+        _check(_lib.nm_q8_weights_dims(self._h, *[ctypes.byref(d) for d in out]))
+        self.c_out, self.k, self.kk, self.n_tiles, self.tile_t = (d.value for d in out)
+
+    @property
+    def handle(self):
+        return self._h
+
+    def free(self):
+        if self._h is not None and self._h.value:
+            _lib.nm_q8_weights_free(self._h)
+        self._h = None
+        self._addr = 0
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def _on_device(t: torch.Tensor):
+    """The tensor's device as the current one (handles are made on, and belong to, the current device)."""
+    return torch.cuda.device(t.device)
+
+
+def nm_q8_prune(w_dense: torch.Tensor, n_keep: int, m_group: int, tile_t: int) -> Q8Weights:
+    """``w_dense``: CUDA fp32 ``[c_out, k]``.  Column-wise N:M pruning as ``nm_prune`` does it, the retained weights in 8-bit
+    integers with a scale for each output channel.  ``n_keep = m_group`` leaves the layer dense."""
+    ptr = _dev_f32(w_dense, "w_dense")
+    if w_dense.dim() != 2:
+        raise TypeError("w_dense must be [c_out, k]")
+    out = ctypes.c_void_p()
+    with _on_device(w_dense):
+        _check(_lib.nm_q8_prune(ptr, *w_dense.shape, n_keep, m_group, tile_t, _stream(), ctypes.byref(out)))
+    return Q8Weights(out.value)
+
+
+def nm_q8_weights_import(values: torch.Tensor, scales: torch.Tensor, indices: torch.Tensor, k: int, n_keep: int, m_group: int,
+                         tile_t: int) -> Q8Weights:
+    """A handle from an already compressed 8-bit layer: ``values [c_out, kk]`` int8, ``scales [c_out]`` fp32,
+    ``indices [n_tiles, kk]`` uint16."""
+    for t, what, dtype, dim in ((values, "values", torch.int8, 2), (indices, "indices", torch.uint16, 2), (scales, "scales", torch.float32, 1)):
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.dim() == dim
+                and t.device == values.device):
+            raise TypeError(f"{what} must be a contiguous {dtype} CUDA tensor of {dim} dimension(s)")
+    c_out = values.shape[0]
+    if n_keep >= 1 and m_group >= n_keep and tile_t >= 1:   # otherwise the library reports the bad argument
+        kk = k // m_group * n_keep + min(k % m_group, n_keep)
+        want = ((values, (c_out, kk)), (scales, (c_out,)), (indices, (-(-c_out // tile_t), kk)))
+        if any(tuple(t.shape) != shape for t, shape in want):
+            raise TypeError("values, scales and indices must be " + ", ".join(str(list(shape)) for _, shape in want)
+                            + f" (got {', '.join(str(list(t.shape)) for t, _ in want)})")
+    out = ctypes.c_void_p()
+    with _on_device(values):
+        _check(_lib.nm_q8_weights_import(values.data_ptr(), scales.data_ptr(), indices.data_ptr(), c_out, k, n_keep, m_group, tile_t,
+                                         _stream(), ctypes.byref(out)))
+    return Q8Weights(out.value)
+
+
+def nm_q8_weights_export(w: Q8Weights):
+    """Returns ``(values [c_out, kk] int8, scales [c_out] fp32, indices [n_tiles, kk] uint16)`` on the current device."""
+    values = torch.empty((w.c_out, w.kk), dtype=torch.int8, device="cuda")
+    scales = torch.empty(w.c_out, dtype=torch.float32, device="cuda")
+    indices = torch.empty((w.n_tiles, w.kk), dtype=torch.uint16, device="cuda")
+    _check(_lib.nm_q8_weights_export(w.handle, values.data_ptr(), scales.data_ptr(), indices.data_ptr(), _stream()))
+    return values, scales, indices
+
+
+def nm_q8_weights_check(w: Q8Weights):
+    _check(_lib.nm_q8_weights_check(w.handle, _stream()))
+
+
+def _q8_out(made):
+    if made.__class__ is int:
+        _check(made)
+    return made
+
+
+def nm_q8_rows(x: torch.Tensor, q: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """Rows (tokens) of ``x`` ``[tokens, h]`` (float32, bfloat16, float16) as 8-bit integers with a scale for each:
+    ``(q [tokens, h] int8, scale [tokens] fp32)``.  A ``q`` allocated here has rows a multiple of 16 bytes apart, as
+    ``nm_q8_linear`` reads them."""
+    return _q8_out(_nm_binding.q8_rows(x, q, scale))
+
+
+def nm_q8_silu_mul(gate: torch.Tensor, up: torch.Tensor, q: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """``up * SiLU(gate)`` in 8 bits, as ``nm_q8_rows``; the two may be the halves of one tensor."""
+    return _q8_out(_nm_binding.q8_rows(gate, up, q, scale))
+
+
+def nm_q8_rmsnorm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None,
+                  residual_out: torch.Tensor | None = None, q: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+    """Root-mean-square norm of ``x`` (plus ``residual``, if given) in 8 bits: ``(q, scale)``, with a residual
+    ``(q, scale, residual_out)`` where ``residual_out`` is the sum in ``x``'s type (it may be ``residual`` or ``x`` itself)."""
+    return _q8_out(_nm_binding.q8_rmsnorm(x, weight, eps, residual, residual_out, q, scale))
+
+
+def nm_q8_linear(w: Q8Weights, xq: torch.Tensor, x_scale: torch.Tensor, bias: torch.Tensor | None = None,
+                 out_dtype: torch.dtype = torch.bfloat16, y: torch.Tensor | None = None) -> torch.Tensor:
+    """Product of 8-bit rows ``xq [tokens, k]`` with the layer's weights: ``[tokens, c_out]`` in ``out_dtype`` (or ``y``'s type)."""
+    return _q8_out(_nm_binding.q8_linear(w._addr, w.c_out, w.k, xq, x_scale, bias, out_dtype, y))
