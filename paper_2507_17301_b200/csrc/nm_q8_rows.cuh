@@ -18,6 +18,7 @@
 #include <cuda_fp16.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "nm_ptx.cuh"
 #include "nm_q8.h"
@@ -81,10 +82,95 @@ __device__ __forceinline__ void store8(T* p, const Eight<T>& e, int n)
         if (i < n) p[i] = e.v[i];
 }
 
-// Relative error of p times 127 / a in 32 bits, with room: four roundings (2.4e-7); for silu_mul the exponential's (at most
-// 2 + 1.173 |g| units of 2^-23, |g| <= 80), the division's (2 units) and three roundings, 1.2e-5.
+// x + r, rounded once: for 16-bit types the two-way addition, which gives what a sum in 32 bits rounded to 16 gives (where that
+// sum is not exact the lesser number is below a quarter of the greater's last place, and both round to the greater).
+template <typename T>
+__device__ __forceinline__ Eight<T> add8(const Eight<T>& x, const Eight<T>& r)
+{
+    Eight<T> s;
+    if constexpr (sizeof(T) == 2) {
+        using T2 = std::conditional_t<std::is_same_v<T, __half>, __half2, __nv_bfloat162>;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            reinterpret_cast<T2*>(&s)[i] = __hadd2_rn(reinterpret_cast<const T2*>(&x)[i], reinterpret_cast<const T2*>(&r)[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s.v[i] = x.v[i] + r.v[i];
+    }
+    return s;
+}
+
+// Two fp32 numbers in a 64-bit register, for the instructions that work on both.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair(float lo, float hi)
+{
+    Pair d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ void split(Pair p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b)
+{
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b)
+{
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// max(|a|, |b|, |c|), NaN if one is.
+__device__ __forceinline__ float top3(float a, float b, float c)
+{
+    float m;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
+// Elements 2i and 2i + 1.
+template <typename T>
+__device__ __forceinline__ Pair two_of(const Eight<T>& e, int i)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        const uint32_t u = reinterpret_cast<const uint32_t*>(&e)[i];
+        return pair(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+    } else {
+        return pair(to_float(e.v[2 * i]), to_float(e.v[2 * i + 1]));
+    }
+}
+
+// Relative error of p times 127 / a in 32 bits, with room: four roundings (2.4e-7); for silu_mul the exponent's two
+// roundings of up to 115 * 2^-24 each (9.5e-6 in all, g >= -80), 2^-22 and 2^-23 of the exponential and the reciprocal, and
+// four roundings.
 template <Q8RowOp OP>
 constexpr float kError = OP == Q8_SILU_MUL ? 1.5e-5f : 4e-7f;
+// silu_mul beyond g = -80: less than kMostProduct * 2^-115 * 80, of which the bound on the row's maximum makes less than 2^-8 of kBorder
+constexpr float kMostProduct = 0x1p20f, kLeastTop = 0x1p-60f;
+constexpr float kMostTop = 0x1p100f;   // (127 p and 1 / a stay normal numbers)
+// How near 127 p / a may come to a border between two integers, beside its own error, before 64 bits decide.
+constexpr float kBorder = 0.5f - 1e-7f;
+
+// The products g u and g u / (1 + exp(-g)): (g u) first, whose underflow cannot matter beside kLeastTop.  Where the exponential
+// or its reciprocal leaves 32 bits (g < -87) the result is 0.
+__device__ __forceinline__ void gated(Pair g, Pair u, Pair* product, Pair* p)
+{
+    float a, b;
+    split(mul2(g, pair(-1.44269504f, -1.44269504f)), a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    split(add2(pair(a, b), pair(1.f, 1.f)), a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    *product = mul2(g, u);
+    *p = mul2(*product, pair(a, b));
+}
 
 // p of one column in 64 bits, from memory.
 template <Q8RowOp OP, typename T, typename W>
@@ -104,16 +190,44 @@ __device__ double exact_value(const Q8Rows& a, size_t row, int col, double* s_ou
 }
 
 template <Q8RowOp OP, typename T, typename W>
-__device__ __noinline__ double exact_again(const Q8Rows& a, size_t row, int col)
+__device__ __forceinline__ bool product_of_non_zeros(const Q8Rows& a, size_t row, int col)
 {
-    return exact_value<OP, T, W>(a, row, col);
+    const float x = to_float(OP == Q8_RMSNORM && a.r ? static_cast<const T*>(a.s)[row * a.s_ld + col] : static_cast<const T*>(a.x)[row * a.x_ld + col]);
+    if constexpr (OP == Q8_SILU_MUL) return x != 0.f && to_float(static_cast<const T*>(a.r)[row * a.r_ld + col]) != 0.f;
+    if constexpr (OP == Q8_RMSNORM) return x != 0.f && to_float(static_cast<const W*>(a.weight)[col]) != 0.f;
+    return x != 0.f;
 }
 
-// u * SiLU(g) where 32 bits do not reach.
-__device__ __noinline__ inline float gated_in_64(float g, float u)
+constexpr float kRound = 12582912.f;   // adding 1.5 * 2^23 rounds to an integer, whose low byte is then the sum's
+
+// Distance of p * inv to the nearest integer plus what its error may add.
+template <Q8RowOp OP>
+__device__ __forceinline__ float border_of(float p, float inv)
 {
-    const double d = g;
-    return static_cast<float>(d / (1.0 + exp(-d)) * static_cast<double>(u));
+    const float whole = fmaf(p, inv, kRound) - kRound;
+    return fmaf(fabsf(whole), kError<OP>, fabsf(fmaf(p, inv, -whole)));
+}
+// One column's integer, which 32 bits left open, in 64 bits; top = 0: |p| itself instead.
+template <Q8RowOp OP, typename T, typename W>
+__device__ __noinline__ double again(const Q8Rows& a, size_t row, int col, double top)
+{
+    const double p = exact_value<OP, T, W>(a, row, col);
+    if (top == 0.0) return fabs(p);
+    a.q[row * a.q_ld + col] = static_cast<int8_t>(rint(127.0 * p / top));
+    return 0.0;
+}
+// Elements of a group for which `f` holds, a bit each.
+template <typename F>
+__device__ __forceinline__ uint32_t which(const Pair (&p)[4], F&& f)
+{
+    uint32_t bits = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        split(p[i], lo, hi);
+        bits |= (f(lo) ? 1u : 0u) << (2 * i) | (f(hi) ? 2u : 0u) << (2 * i);
+    }
+    return bits;
 }
 
 struct Scratch {
@@ -144,8 +258,25 @@ __device__ __forceinline__ double row_max(double v, double* part)
 
 // The whole row in 64 bits (its thread `t` of TPR; all of them come here together).
 template <Q8RowOp OP, typename T, typename W, int TPR>
-__device__ __noinline__ void row_in_64(const Q8Rows& a, size_t row, int t, Scratch* sc)
+__device__ __noinline__ void row_in_64(const Q8Rows& a, size_t row, int t, bool zero, Scratch* sc)
 {
+    if (zero) {
+        // every product is 0 in 32 bits: usually a row of padding.  It is one of zeros if every product has a factor 0
+        int some = 0;
+        for (int v = t; v * 8 < a.h; v += TPR)
+            for (int c = v * 8; c < min(v * 8 + 8, a.h); ++c) some |= product_of_non_zeros<OP, T, W>(a, row, c);
+        if constexpr (TPR > 32) some = __syncthreads_or(some);
+        else some = __any_sync(0xFFFFFFFFu, some);
+        if (!some) {
+            if (t == 0) a.scale[row] = 0.f;
+            for (int v = t; v * 8 < a.h; v += TPR) {
+                int8_t* q = a.q + row * a.q_ld + v * 8;
+                if (a.h - v * 8 >= 8) *reinterpret_cast<uint2*>(q) = make_uint2(0u, 0u);
+                else for (int c = 0; c < a.h - v * 8; ++c) q[c] = 0;
+            }
+            return;
+        }
+    }
     double top = 0.0, sum = 0.0;
     int bad = 0;
     for (int v = t; v * 8 < a.h; v += TPR)
@@ -186,64 +317,118 @@ __device__ __noinline__ void row_in_64(const Q8Rows& a, size_t row, int t, Scrat
 }
 
 // TPR threads take a row, each NV groups of eight columns, in steps of TPR groups.  KEEP: the row's p stay in registers (8 * NV * TPR >= h).
+// (at least 768 threads an SM)
 template <Q8RowOp OP, typename T, typename W, int TPR, int NV, bool KEEP, bool VEC>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) k_q8_rows(const __grid_constant__ Q8Rows a)
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 768 ? 1 : 768 / TPR) k_q8_rows(const __grid_constant__ Q8Rows a)
 {
     constexpr int ROWS = TPR < 128 ? 128 / TPR : 1;
     static_assert(TPR == 32 || ROWS == 1, "a row is a warp's or a block's");
     // products of two 16-bit values fit 32 bits, an input is itself
     constexpr bool EXACT = OP == Q8_ROWS || (OP == Q8_RMSNORM && sizeof(T) == 2 && sizeof(W) == 2);
-    __shared__ Scratch scratch[ROWS];
+    // p of at most 16 bits: 127 p is exact in 32, and 127 p / a is a half or further from it than fp32's half a place: 254 p - (2k + 1) a
+    // is a multiple of p's last place, more than 2^-16 p, and that over 2 a is more than 2^-24 of the quotient
+    constexpr bool DIVIDE = sizeof(T) == 2 && (OP == Q8_ROWS || (OP == Q8_RMSNORM && std::is_same_v<T, __nv_bfloat16> && sizeof(W) == 2));
+    constexpr bool ASYNC = KEEP && VEC;
+    extern __shared__ uint4 smem[];
+    __shared__ Scratch scratch[2];   // rows take turns: a row's is written after the barrier behind the last reading of it
     const int t = threadIdx.x % TPR;
-    const size_t row = static_cast<size_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    const size_t tokens = static_cast<size_t>(a.tokens), step = static_cast<size_t>(gridDim.x) * ROWS;
+    const W* weight = static_cast<const W*>(a.weight);
     nmk::pdl_launch_dependents();
     nmk::pdl_wait();
-    if (row >= static_cast<size_t>(a.tokens)) return;   // (whole rows: ROWS > 1 has no barrier across warps)
-    Scratch* sc = scratch + threadIdx.x / TPR;
+    // ASYNC: a thread copies its part of the next row into places of its own in shared memory while this row is reduced and written
+    // (no barrier, no registers; two sets of places taken in turn)
+    constexpr int PIECES = sizeof(T) / 2, THREADS = TPR < 128 ? 128 : TPR;
+    const bool two = OP == Q8_SILU_MUL || (OP == Q8_RMSNORM && a.r != nullptr);
+    const uint32_t places = nmk::smem_u32(smem) + threadIdx.x * 16u;
+    auto place = [&](int turn, int tensor, int i, int piece) {
+        return places + static_cast<uint32_t>((((turn * (two ? 2 : 1) + tensor) * NV + i) * PIECES + piece) * THREADS) * 16u;
+    };
+    auto fetch = [&](size_t row, int turn) {
+        const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
+        const T* r = static_cast<const T*>(a.r) + row * a.r_ld;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = t + i * TPR;
+            if (v * 8 >= a.h) continue;
+#pragma unroll
+            for (int piece = 0; piece < PIECES; ++piece) {
+                // zeros behind the last column (of a group of fp32 numbers the second piece may be all behind it: nothing is read then)
+                const int bytes = (a.h - v * 8) * static_cast<int>(sizeof(T)) - piece * 16;
+                const uint32_t some = bytes < 16 ? (bytes > 0 ? bytes : 0) : 16;
+                const int from = some ? v * 8 + piece * (16 / static_cast<int>(sizeof(T))) : 0;
+                nmk::cp_async16(place(turn, 0, i, piece), x + from, some);
+                if (two) nmk::cp_async16(place(turn, 1, i, piece), r + from, some);
+            }
+        }
+    };
+    auto fetched = [&](int turn, int tensor, int i) {
+        Eight<T> e;
+#pragma unroll
+        for (int piece = 0; piece < PIECES; ++piece) {
+            uint4 u;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(turn, tensor, i, piece)) : "memory");
+            reinterpret_cast<uint4*>(&e)[piece] = u;
+        }
+        return e;
+    };
+    // (whole rows leave: ROWS > 1 has no barrier across warps)
+    size_t row = static_cast<size_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    if constexpr (ASYNC) {
+        if (row < tokens) fetch(row, 0);
+        nmk::cp_async_commit();
+    }
+    const size_t first_row = row;
+    bool set_aside = false;
+    for (int turn = 0; row < tokens; row += step, turn ^= 1) {
+    Scratch* sc = scratch + turn;
     const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
     const T* r = a.r ? static_cast<const T*>(a.r) + row * a.r_ld : nullptr;
     T* s_row = a.s ? static_cast<T*>(a.s) + row * a.s_ld : nullptr;
-    const W* weight = static_cast<const W*>(a.weight);
 
-    float p[KEEP ? NV : 1][8];
-    float sum = 0.f;
-    uint32_t top = 0u;   // bits of max |p|: NaN above infinity above numbers
-    // p of the groups at `base` on; `first`: sums, and the residual's addition is written
-    auto values = [&](int v, float (&out)[8], const Eight<T>& ex, const Eight<T>& er, const Eight<W>& ew, bool first) {
-        const int n = a.h - v * 8;
+    Pair p[KEEP ? NV : 1][4];
+    Pair sum2 = 0;
+    float top = 0.f;   // max |p|, NaN if one is
+    // p of the group `v`; `first`: sums, and the residual's addition is written
+    auto values = [&](int v, Pair (&out)[4], const Eight<T>& ex, const Eight<T>& er, const Eight<W>& ew, bool first) {
         if constexpr (OP == Q8_RMSNORM) {
             Eight<T> es = ex;
-            if (r && first) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) es.v[i] = from_float<T>(to_float(ex.v[i]) + to_float(er.v[i]));
-                store8<T, VEC>(s_row + v * 8, es, n);
+            if (two && first) {
+                es = add8<T>(ex, er);
+                store8<T, VEC>(s_row + v * 8, es, a.h - v * 8);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float s = to_float(es.v[i]);
-                if (first) sum = fmaf(s, s, sum);
-                out[i] = s * to_float(ew.v[i]);
+            for (int i = 0; i < 4; ++i) {
+                const Pair s = two_of(es, i);
+                if (first) sum2 = fma2(s, s, sum2);
+                out[i] = mul2(s, two_of(ew, i));
             }
         } else if constexpr (OP == Q8_SILU_MUL) {
+            float most = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float g = to_float(ex.v[i]), u = to_float(er.v[i]);
-                out[i] = __fdividef(g, 1.f + __expf(-g)) * u;
-                // outside the range of the error bound: exp(-g) overflows, or g is next to the least number
-                if (g < -80.f || (fabsf(g) < 1e-30f && g != 0.f)) out[i] = gated_in_64(g, u);
+            for (int i = 0; i < 4; ++i) {
+                Pair product;
+                gated(two_of(ex, i), two_of(er, i), &product, &out[i]);
+                float lo, hi;
+                split(product, lo, hi);
+                most = top3(most, lo, hi);
             }
+            if (!(most <= kMostProduct)) top = NAN;   // (the row goes to 64 bits)
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = to_float(ex.v[i]);
+            for (int i = 0; i < 4; ++i) out[i] = two_of(ex, i);
         }
         if (first) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(out[i]) & 0x7FFFFFFFu);   // (columns past the end are zeros)
+            for (int i = 0; i < 4; ++i) {   // (columns past the end are zeros)
+                float lo, hi;
+                split(out[i], lo, hi);
+                top = top3(top, lo, hi);
+            }
         }
     };
     auto pass = [&](int base, bool first, auto&& use) {
         Eight<T> ex[NV], er[NV];
-        Eight<W> ew[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = base + i * TPR, n = a.h - v * 8;
@@ -252,64 +437,94 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) k_q8_rows(const __grid_
             const T* from = OP == Q8_RMSNORM && r && !first ? s_row : x;
             ex[i] = load8<T, VEC>(from + v * 8, n);
             if (OP == Q8_SILU_MUL || (OP == Q8_RMSNORM && r && first)) er[i] = load8<T, VEC>(r + v * 8, n);
-            if (OP == Q8_RMSNORM) ew[i] = load8<W, VEC>(weight + v * 8, n);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = base + i * TPR;
             if (v * 8 >= a.h) continue;
-            float tmp[8];
-            values(v, tmp, ex[i], er[i], ew[i], first);
+            Eight<W> ew;
+            if (OP == Q8_RMSNORM) ew = load8<W, VEC>(weight + v * 8, a.h - v * 8);   // (out of the L1: every row reads them)
+            Pair tmp[4];
+            values(v, tmp, ex[i], er[i], ew, first);
             use(i, v, tmp);
         }
     };
-    if constexpr (KEEP) {
-        pass(t, true, [&](int i, int, float (&f)[8]) {
+    if constexpr (ASYNC) {
+        if (row + step < tokens) fetch(row + step, turn ^ 1);
+        nmk::cp_async_commit();
+        nmk::cp_async_wait<1>();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[i][e] = f[e];
+        for (int i = 0; i < NV; ++i) {
+            const int v = t + i * TPR;
+            Eight<T> er = {};
+            Eight<W> ew = {};
+            if (v * 8 >= a.h) continue;
+            if (OP == Q8_RMSNORM) ew = load8<W, VEC>(weight + v * 8, a.h - v * 8);   // (out of the L1: every row reads them)
+            if (two) er = fetched(turn, 1, i);
+            values(v, p[i], fetched(turn, 0, i), er, ew, true);
+        }
+    } else if constexpr (KEEP) {
+        pass(t, true, [&](int i, int, Pair (&f)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[i][e] = f[e];
         });
     } else {
-        for (int base = t; base * 8 < a.h; base += NV * TPR) pass(base, true, [](int, int, float (&)[8]) {});
+        for (int base = t; base * 8 < a.h; base += NV * TPR) pass(base, true, [](int, int, Pair (&)[4]) {});
     }
 
+    float sum = 0.f;
     if constexpr (OP == Q8_RMSNORM) {
+        float lo, hi;
+        split(sum2, lo, hi);
+        sum = lo + hi;
         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
     }
-    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    // as bits: NaN above infinity above numbers
+    uint32_t top_bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top) & 0x7FFFFFFFu);
     if constexpr (TPR > 32) {
         if ((t & 31) == 0) {
             sc->sum[t >> 5] = sum;
-            sc->top[t >> 5] = top;
+            sc->top[t >> 5] = top_bits;
         }
         __syncthreads();
         const int lane = t & 31;
-        top = __reduce_max_sync(0xFFFFFFFFu, lane < TPR / 32 ? sc->top[lane] : 0u);
+        top_bits = __reduce_max_sync(0xFFFFFFFFu, lane < TPR / 32 ? sc->top[lane] : 0u);
         if constexpr (OP == Q8_RMSNORM) {
             sum = lane < TPR / 32 ? sc->sum[lane] : 0.f;
             for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
         }
     }
-    const float a32 = __uint_as_float(top);
-    // 2^-60: products that 32 bits lose below 2^-126 are then less than a step by far
-    if (!(a32 >= 0x1p-60f && a32 < INFINITY && sum < INFINITY)) {
-        row_in_64<OP, T, W, TPR>(a, row, t, sc);
-        return;
+    const float a32 = __uint_as_float(top_bits);
+    // kLeastTop: what 32 bits lose below 2^-126 is then less than a step by far
+    if (!(a32 >= kLeastTop && a32 <= kMostTop && sum < INFINITY)) {
+        // (after the others: a call in here would cost the loop registers)
+        set_aside = true;
+        if (t == 0) a.scale[row] = a32 == 0.f ? -2.f : -1.f;
+        continue;
     }
     double a64 = a32;
     if constexpr (!EXACT) {
-        double mine = 0.0;
         const float near_top = a32 * (1.f - 2.f * kError<OP>);
-        auto look = [&](int, int v, float (&f)[8]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (fabsf(f[e]) >= near_top) mine = fmax(mine, fabs(exact_again<OP, T, W>(a, row, v * 8 + e)));
+        double mine = 0.0;
+        auto is_near = [&](float v) { return fabsf(v) >= near_top; };
+        // (KEEP: one loop over all groups' bits, so that there is one call; a lane or two of the row have any)
+        auto look = [&](uint32_t bits, int v0) {
+            for (; bits; bits &= bits - 1u) {
+                const int at = __ffs(bits) - 1;
+                mine = fmax(mine, again<OP, T, W>(a, row, (v0 + at / 8 * TPR) * 8 + at % 8, 0.0));
+            }
         };
-        if constexpr (KEEP) {
+        if (top < near_top) {
+            // none of this thread's
+        } else if constexpr (KEEP) {
+            uint32_t bits = 0u;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if ((t + i * TPR) * 8 < a.h) look(i, t + i * TPR, p[i]);
+                if ((t + i * TPR) * 8 < a.h) bits |= which(p[i], is_near) << (8 * i);
+            look(bits, t);
         } else {
-            for (int base = t; base * 8 < a.h; base += NV * TPR) pass(base, false, look);
+            for (int base = t; base * 8 < a.h; base += NV * TPR)
+                pass(base, false, [&](int, int v, Pair (&f)[4]) { look(which(f, is_near), v); });
         }
         a64 = row_max<TPR>(mine, sc->a);
     }
@@ -320,70 +535,125 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) k_q8_rows(const __grid_
     }
     const float inv = 127.f / static_cast<float>(a64);
     int8_t* q_row = a.q + row * a.q_ld;
-    auto quantise = [&](int, int v, float (&f)[8]) {
-        int k[8];
-        bool again = false;
+    const float a32_top = static_cast<float>(a64);
+    // q of the group `v`; a bit for each that 64 bits have to decide
+    auto quantise = [&](int v, Pair (&f)[4]) {
+        uint32_t k[8];
+        float border = 0.f;
+        if constexpr (DIVIDE) {
+            // 127 p / a, rounded correctly (Markstein: a quotient from the reciprocal, its remainder by fma, one correction), and
+            // that to an integer: a quotient between two halves keeps its side, a tie is exact (see DIVIDE)
+            const float rcp = 1.f / a32_top;
+            const Pair r = pair(rcp, rcp), minus_a = pair(-a32_top, -a32_top);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = f[e] * inv, n = rintf(y);
-            k[e] = static_cast<int>(n);
-            again |= fabsf(y - n) > 0.5f - fabsf(y) * kError<OP>;
-        }
-        if (again) {
+            for (int i = 0; i < 4; ++i) {
+                const Pair t = mul2(f[i], pair(127.f, 127.f)), y = mul2(t, r);
+                const Pair n = add2(fma2(fma2(y, minus_a, t), r, y), pair(kRound, kRound));
+                float lo, hi;
+                split(n, lo, hi);
+                k[2 * i] = __float_as_uint(lo);
+                k[2 * i + 1] = __float_as_uint(hi);
+            }
+        } else {
+            // n = the nearest integer to p * inv, and how far off that is: within the error bound of a half, 64 bits decide
+            const Pair by = pair(inv, inv);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = f[e] * inv;
-                if (fabsf(y - rintf(y)) > 0.5f - fabsf(y) * kError<OP>) {
-                    const double d = EXACT ? static_cast<double>(f[e]) : exact_again<OP, T, W>(a, row, v * 8 + e);
-                    k[e] = static_cast<int>(rint(127.0 * d / a64));
-                }
+            for (int i = 0; i < 4; ++i) {
+                const Pair n = fma2(f[i], by, pair(kRound, kRound)), minus = fma2(n, pair(-1.f, -1.f), pair(kRound, kRound)), off = fma2(f[i], by, minus);
+                float n0, n1, m0, m1, d0, d1;
+                split(n, n0, n1);
+                split(minus, m0, m1);
+                split(off, d0, d1);
+                k[2 * i] = __float_as_uint(n0);
+                k[2 * i + 1] = __float_as_uint(n1);
+                border = top3(border, fmaf(fabsf(m0), kError<OP>, fabsf(d0)), fmaf(fabsf(m1), kError<OP>, fabsf(d1)));
             }
         }
-        uint32_t lo = 0u, hi = 0u;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            lo |= (static_cast<uint32_t>(k[e]) & 0xFFu) << (8 * e);
-            hi |= (static_cast<uint32_t>(k[e + 4]) & 0xFFu) << (8 * e);
-        }
+        const uint32_t lo = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
+        const uint32_t hi = __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410);
         const int n = a.h - v * 8;
         if (n >= 8) {
             *reinterpret_cast<uint2*>(q_row + v * 8) = make_uint2(lo, hi);
         } else {
             for (int e = 0; e < n; ++e) q_row[v * 8 + e] = static_cast<int8_t>((e < 4 ? lo >> (8 * e) : hi >> (8 * (e - 4))) & 0xFFu);
         }
+        return border > kBorder ? which(f, [&](float p) { return border_of<OP>(p, inv) > kBorder; }) : 0u;
+    };
+    auto decide = [&](uint32_t bits, int v0) {
+        for (; bits; bits &= bits - 1u) {
+            const int at = __ffs(bits) - 1, col = (v0 + at / 8 * TPR) * 8 + at % 8;
+            if (col < a.h) again<OP, T, W>(a, row, col, a64);
+        }
     };
     if constexpr (KEEP) {
+        uint32_t open = 0u;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if ((t + i * TPR) * 8 < a.h) quantise(i, t + i * TPR, p[i]);
+            if ((t + i * TPR) * 8 < a.h) open |= quantise(t + i * TPR, p[i]) << (8 * i);
+        if constexpr (!DIVIDE) decide(open, t);
     } else {
-        for (int base = t; base * 8 < a.h; base += NV * TPR) pass(base, false, quantise);
+        for (int base = t; base * 8 < a.h; base += NV * TPR)
+            pass(base, false, [&](int, int v, Pair (&f)[4]) {
+                const uint32_t open = quantise(v, f);
+                if constexpr (!DIVIDE) decide(open, v);
+            });
+    }
+    }
+    if (!set_aside) return;
+    if constexpr (TPR > 32) __syncthreads();
+    else __syncwarp();
+    for (row = first_row; row < tokens; row += step) {
+        const float mark = *reinterpret_cast<volatile float*>(a.scale + row);
+        if constexpr (TPR > 32) __syncthreads();   // (its first thread replaces the mark, and the scratch is used again)
+        else __syncwarp();
+        if (mark < 0.f) row_in_64<OP, T, W, TPR>(a, row, t, mark == -2.f, scratch);
     }
 }
 
 template <Q8RowOp OP, typename T, typename W, int TPR, int NV, bool KEEP, bool VEC>
 cudaError_t launch_one(const Q8Rows& a, cudaStream_t st)
 {
-    constexpr int rows = TPR < 128 ? 128 / TPR : 1;
-    return nmhost::launch_pdl(k_q8_rows<OP, T, W, TPR, NV, KEEP, VEC>, static_cast<unsigned>((a.tokens + rows - 1) / rows), TPR < 128 ? 128u : TPR, 0,
-                              st, a);
+    constexpr int rows = TPR < 128 ? 128 / TPR : 1, threads = TPR < 128 ? 128 : TPR;
+    const int blocks = (a.tokens + rows - 1) / rows;
+    // two rows' places of each thread, of one or two tensors; as many blocks as an SM holds for certain (768 threads, 227 KB)
+    const size_t smem = KEEP && VEC ? static_cast<size_t>(threads) * NV * 8 * sizeof(T) * 2 * (a.r ? 2 : 1) : 0;
+    int resident = threads > 768 ? 1 : 768 / threads;
+    if (smem && 225 * 1024 / (smem + 3072) < static_cast<size_t>(resident)) resident = static_cast<int>(225 * 1024 / (smem + 3072));
+    resident *= nmhost::sm_count();
+    auto kernel = k_q8_rows<OP, T, W, TPR, NV, KEEP, VEC>;
+    const cudaError_t e = nmhost::ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
+    if (e != cudaSuccess) return e;
+    return nmhost::launch_pdl(kernel, static_cast<unsigned>(blocks < resident ? blocks : resident), static_cast<unsigned>(threads), smem, st, a);
 }
 
-// Threads for a row: four groups of eight columns each, one or two where there are too few rows to fill the GPU.
+// Threads for a row: two groups of eight columns each, one where there are too few rows to fill the GPU.
 template <Q8RowOp OP, typename T, typename W>
 cudaError_t launch_shape(const Q8Rows& a, bool vec, cudaStream_t st)
 {
     if (!vec) {
-        if (a.h <= 1024) return launch_one<OP, T, W, 32, 4, true, false>(a, st);
-        if (a.h <= 8192) return launch_one<OP, T, W, 256, 4, true, false>(a, st);
-        return launch_one<OP, T, W, 512, 4, false, false>(a, st);
+        if (a.h <= 512) return launch_one<OP, T, W, 32, 2, true, false>(a, st);
+        if (a.h <= 4096) return launch_one<OP, T, W, 256, 2, true, false>(a, st);
+        return launch_one<OP, T, W, 512, 2, false, false>(a, st);
     }
     const bool few = a.tokens <= 2 * nmhost::sm_count();
-    if (a.h <= 1024 && !few) return launch_one<OP, T, W, 32, 4, true, true>(a, st);
-    if (a.h <= 4096) return few ? launch_one<OP, T, W, 512, 1, true, true>(a, st) : launch_one<OP, T, W, 128, 4, true, true>(a, st);
-    if (a.h <= 8192 && !few) return launch_one<OP, T, W, 256, 4, true, true>(a, st);
-    if (a.h <= 16384) return few ? launch_one<OP, T, W, 1024, 2, true, true>(a, st) : launch_one<OP, T, W, 512, 4, true, true>(a, st);
-    return launch_one<OP, T, W, 512, 4, false, true>(a, st);
+    if (a.h <= 512) return launch_one<OP, T, W, 32, 2, true, true>(a, st);
+    if (a.h <= 2048 && !few) return launch_one<OP, T, W, 128, 2, true, true>(a, st);
+    if (few) {
+        if (a.h <= 4096) return launch_one<OP, T, W, 512, 1, true, true>(a, st);
+        if (a.h <= 8192) return launch_one<OP, T, W, 1024, 1, true, true>(a, st);
+    }
+    // (32-bit numbers: half as many in the same places, and 16384 columns of two tensors would not fit)
+    if constexpr (sizeof(T) == 4) {
+        if (a.h <= 4096) return launch_one<OP, T, W, 256, 2, true, true>(a, st);
+        if (a.h <= 8192) return launch_one<OP, T, W, 512, 2, true, true>(a, st);
+    } else {
+        if (few && a.h <= 16384) return launch_one<OP, T, W, 1024, 2, true, true>(a, st);
+        if (a.h <= 4096) return launch_one<OP, T, W, 128, 4, true, true>(a, st);
+        if (a.h <= 8192) return launch_one<OP, T, W, 256, 4, true, true>(a, st);
+        if (a.h <= 12288) return launch_one<OP, T, W, 384, 4, true, true>(a, st);
+        if (a.h <= 16384) return launch_one<OP, T, W, 512, 4, true, true>(a, st);
+    }
+    return launch_one<OP, T, W, 512, 2, false, true>(a, st);
 }
 
 template <typename T>
