@@ -172,13 +172,26 @@ __device__ __forceinline__ void gated(Pair g, Pair u, Pair* product, Pair* p)
     *p = mul2(*product, pair(a, b));
 }
 
+__device__ __forceinline__ double gated_in_64(double g, double u) { return g / (1.0 + exp(-g)) * u; }
+template <typename T>
+__device__ __forceinline__ T shared_element(uint32_t at)
+{
+    T v;
+    if constexpr (sizeof(T) == 4) {
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(reinterpret_cast<float&>(v)) : "r"(at) : "memory");
+    } else {
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(reinterpret_cast<uint16_t&>(v)) : "r"(at) : "memory");
+    }
+    return v;
+}
+
 // p of one column in 64 bits, from memory.
 template <Q8RowOp OP, typename T, typename W>
 __device__ double exact_value(const Q8Rows& a, size_t row, int col, double* s_out = nullptr)
 {
     if constexpr (OP == Q8_SILU_MUL) {
         const double g = to_float(static_cast<const T*>(a.x)[row * a.x_ld + col]), u = to_float(static_cast<const T*>(a.r)[row * a.r_ld + col]);
-        return g / (1.0 + exp(-g)) * u;
+        return gated_in_64(g, u);
     } else if constexpr (OP == Q8_ROWS) {
         return to_float(static_cast<const T*>(a.x)[row * a.x_ld + col]);
     } else {
@@ -207,11 +220,25 @@ __device__ __forceinline__ float border_of(float p, float inv)
     const float whole = fmaf(p, inv, kRound) - kRound;
     return fmaf(fabsf(whole), kError<OP>, fabsf(fmaf(p, inv, -whole)));
 }
-// One column's integer, which 32 bits left open, in 64 bits; top = 0: |p| itself instead.
+// One column's integer, which 32 bits left open, in 64 bits; top = 0: |p| itself instead.  x_at, r_at: where the column's inputs
+// lie in shared memory (0: read them from global memory, which takes longer).
 template <Q8RowOp OP, typename T, typename W>
-__device__ __noinline__ double again(const Q8Rows& a, size_t row, int col, double top)
+__device__ __noinline__ double again(const Q8Rows& a, size_t row, int col, uint32_t x_at, uint32_t r_at, double top)
 {
-    const double p = exact_value<OP, T, W>(a, row, col);
+    double p;
+    if (x_at == 0u) {
+        p = exact_value<OP, T, W>(a, row, col);
+    } else {
+        const T x = shared_element<T>(x_at);
+        if constexpr (OP == Q8_RMSNORM) {
+            const T s = a.r ? from_float<T>(to_float(x) + to_float(shared_element<T>(r_at))) : x;
+            p = static_cast<double>(to_float(s)) * static_cast<double>(to_float(static_cast<const W*>(a.weight)[col]));
+        } else if constexpr (OP == Q8_SILU_MUL) {
+            p = gated_in_64(to_float(x), to_float(shared_element<T>(r_at)));
+        } else {
+            p = to_float(x);
+        }
+    }
     if (top == 0.0) return fabs(p);
     a.q[row * a.q_ld + col] = static_cast<int8_t>(rint(127.0 * p / top));
     return 0.0;
@@ -502,6 +529,10 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         if (t == 0) a.scale[row] = a32 == 0.f ? -2.f : -1.f;
         continue;
     }
+    // (element `at` of this thread's part: group at / 8, column at % 8 of it)
+    auto input_at = [&](int tensor, int at) {
+        return ASYNC ? place(turn, two ? tensor : 0, at / 8, at % 8 / (8 / PIECES)) + static_cast<uint32_t>(at % (8 / PIECES) * sizeof(T)) : 0u;
+    };
     double a64 = a32;
     if constexpr (!EXACT) {
         const float near_top = a32 * (1.f - 2.f * kError<OP>);
@@ -511,7 +542,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         auto look = [&](uint32_t bits, int v0) {
             for (; bits; bits &= bits - 1u) {
                 const int at = __ffs(bits) - 1;
-                mine = fmax(mine, again<OP, T, W>(a, row, (v0 + at / 8 * TPR) * 8 + at % 8, 0.0));
+                mine = fmax(mine, again<OP, T, W>(a, row, (v0 + at / 8 * TPR) * 8 + at % 8, input_at(0, at), input_at(1, at), 0.0));
             }
         };
         if (top < near_top) {
@@ -582,7 +613,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     auto decide = [&](uint32_t bits, int v0) {
         for (; bits; bits &= bits - 1u) {
             const int at = __ffs(bits) - 1, col = (v0 + at / 8 * TPR) * 8 + at % 8;
-            if (col < a.h) again<OP, T, W>(a, row, col, a64);
+            if (col < a.h) again<OP, T, W>(a, row, col, input_at(0, at), input_at(1, at), a64);
         }
     };
     if constexpr (KEEP) {
