@@ -397,7 +397,8 @@ nm_status_t nm_q8_prune(const float* w_dense, int c_out, int k, int n_keep, int 
  */
 nm_status_t nm_q8_weights_import(const int8_t* values, const float* scales, const uint16_t* indices, int c_out, int k,
                                  int n_keep, int m_group, int tile_t, void* cuda_stream, nm_q8_weights_t** out);
-/* Copies the canonical form to caller memory on `cuda_stream`; any pointer may be NULL. */
+/* Copies the canonical form to caller memory on `cuda_stream`; any pointer may be NULL.  `values` lies on the handle's device, which is
+ * the current one. */
 nm_status_t nm_q8_weights_export(const nm_q8_weights_t* w, int8_t* values, float* scales, uint16_t* indices,
                                  void* cuda_stream);
 nm_status_t nm_q8_weights_dims(const nm_q8_weights_t* w, int* c_out, int* k, int* kk, int* n_tiles, int* tile_t);

@@ -89,7 +89,7 @@ struct OnDevice {   // makes a handle's device the current one for as long as th
     OnDevice& operator=(const OnDevice&) = delete;
 };
 
-// One row's retained weights to 8 bits.
+// One row's retained weights to 8 bits: values [c_out][kk].
 __global__ void __launch_bounds__(256) k_q8_quantise(const float* __restrict__ w, int k, int kk, int kk_ld, int tile_t, const uint16_t* __restrict__ idx,
                                                      int8_t* __restrict__ values, float* __restrict__ scales)
 {
@@ -106,30 +106,40 @@ __global__ void __launch_bounds__(256) k_q8_quantise(const float* __restrict__ w
     const bool good = top < 0x7F800000u;
     const double a = __uint_as_float(top);
     if (threadIdx.x == 0) scales[o] = good ? static_cast<float>(a / 127.0) : NAN;
-    for (int j = threadIdx.x; j < kk_ld; j += 256)
-        values[static_cast<size_t>(o) * kk_ld + j] =
-            j < kk && good && top ? static_cast<int8_t>(rint(127.0 * static_cast<double>(row[col[j]]) / a)) : static_cast<int8_t>(0);
+    for (int j = threadIdx.x; j < kk; j += 256)
+        values[static_cast<size_t>(o) * kk + j] = good && top ? static_cast<int8_t>(rint(127.0 * static_cast<double>(row[col[j]]) / a)) : static_cast<int8_t>(0);
 }
 
-// The handle's arrays from an index array and retained values (either may already be the handle's own).  A block writes 64 rows
-// of a 128-column block of the expanded form; the blocks of the first column block also copy values and indices.  `bad` is set
-// for an index row that is not strictly ascending below k with N columns per group; such a handle is thrown away.
-__global__ void __launch_bounds__(256) k_q8_layout(const int8_t* __restrict__ values, const uint16_t* __restrict__ idx, int ld, const nm_q8_weights h,
-                                                   int* __restrict__ bad)
+// The handle's copy of given index rows.  `bad` is set for one that is not strictly ascending below k with N columns per group; such a
+// handle is thrown away.
+__global__ void __launch_bounds__(256) k_q8_indices(const uint16_t* __restrict__ idx, const nm_q8_weights h, int* __restrict__ bad)
+{
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j >= h.kk_ld) return;
+    for (int tile = blockIdx.y; tile < h.n_tiles; tile += gridDim.y) {
+        const uint16_t* row = idx + static_cast<size_t>(tile) * h.kk;
+        const int c = j < h.kk ? row[j] : 0;
+        if (j < h.kk && (c >= h.k || (j > 0 && c <= row[j - 1]) || c / h.m_group != j / h.n_keep)) *bad = 1;
+        h.indices[static_cast<size_t>(tile) * h.kk_ld + j] = static_cast<uint16_t>(c);
+    }
+}
+
+// Expanded form from the handle's indices and values [c_out][kk]: a block writes 64 rows of a 128-column block.  (Index rows out of
+// order give a wrong place, never one outside a row.)
+__global__ void __launch_bounds__(256) k_q8_expand(const int8_t* __restrict__ values, const nm_q8_weights h)
 {
     __shared__ int s_pos[128];   // place of a column among the tile's retained ones, -1: pruned
     const int kb = blockIdx.x, row0 = blockIdx.y * 64;
-    int tile = -1;
     for (int r0 = row0; r0 < row0 + 64 && r0 < h.rows;) {
         // rows of one tile at a time
-        tile = r0 < h.c_out ? r0 / h.tile_t : -1;
-        int r1 = r0 < h.c_out ? min(min((tile + 1) * h.tile_t, h.c_out), row0 + 64) : row0 + 64;
+        const int tile = r0 < h.c_out ? r0 / h.tile_t : -1;
+        const int r1 = r0 < h.c_out ? min(min((tile + 1) * h.tile_t, h.c_out), row0 + 64) : row0 + 64;
         __syncthreads();
         if (threadIdx.x < 128) {
             const int c = kb * 128 + threadIdx.x;
             int pos = -1;
             if (tile >= 0 && c < h.k) {
-                const uint16_t* row = idx + static_cast<size_t>(tile) * ld;
+                const uint16_t* row = h.indices + static_cast<size_t>(tile) * h.kk_ld;
                 int lo = 0, hi = h.kk;
                 while (lo < hi) {
                     const int mid = (lo + hi) / 2;
@@ -148,27 +158,44 @@ __global__ void __launch_bounds__(256) k_q8_layout(const int8_t* __restrict__ va
 #pragma unroll
                 for (int b = 0; b < 16; ++b) {
                     const int pos = s_pos[piece * 16 + b];
-                    if (pos >= 0) word[b / 4] |= (static_cast<uint32_t>(values[static_cast<size_t>(r) * ld + pos]) & 0xFFu) << (8 * (b % 4));
+                    if (pos >= 0) word[b / 4] |= (static_cast<uint32_t>(values[static_cast<size_t>(r) * h.kk + pos]) & 0xFFu) << (8 * (b % 4));
                 }
             }
             uint8_t* dst = reinterpret_cast<uint8_t*>(h.expanded) + (static_cast<size_t>(kb) * h.rows + r) * 128 + ((piece ^ (r & 7)) << 4);
             *reinterpret_cast<uint4*>(dst) = make_uint4(word[0], word[1], word[2], word[3]);
         }
-        if (kb == 0 && tile >= 0) {
-            for (int r = r0; r < r1; ++r) {
-                if (values != h.values)
-                    for (int j = threadIdx.x; j < h.kk_ld; j += 256)
-                        h.values[static_cast<size_t>(r) * h.kk_ld + j] = j < h.kk ? values[static_cast<size_t>(r) * ld + j] : static_cast<int8_t>(0);
-                if (r == tile * h.tile_t)
-                    for (int j = threadIdx.x; j < h.kk_ld; j += 256) {
-                        const int c = j < h.kk ? idx[static_cast<size_t>(tile) * ld + j] : 0;
-                        const int before = j > 0 && j < h.kk ? idx[static_cast<size_t>(tile) * ld + j - 1] : -1;
-                        if (j < h.kk && (c >= h.k || c <= before || c / h.m_group != j / h.n_keep)) *bad = 1;
-                        h.indices[static_cast<size_t>(tile) * h.kk_ld + j] = static_cast<uint16_t>(c);
-                    }
-            }
-        }
         r0 = r1;
+    }
+}
+
+int packed_tile(const nm_q8_weights& h) { return h.n_keep == h.m_group ? h.c_out : h.tile_t; }
+
+// Packed form from values [c_out][kk]: a warp writes a unit's 512 bytes of 64 columns.
+__global__ void __launch_bounds__(256) k_q8_pack(const int8_t* __restrict__ values, const nm_q8_weights h, int tile_t)
+{
+    const int chunks = h.kk_ld / 64, c = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (c >= chunks) return;
+    const int n_units = (h.c_out + tile_t - 1) / tile_t * h.units;
+    for (int u = blockIdx.y; u < n_units; u += gridDim.y) {
+        const int in_tile = u % h.units * 8 + (lane >> 2), o = u / h.units * tile_t + in_tile, j0 = c * 64 + (lane & 3) * 16;
+        uint32_t word[4] = {0u, 0u, 0u, 0u};
+        if (in_tile < tile_t && o < h.c_out) {
+#pragma unroll
+            for (int b = 0; b < 16; ++b)
+                if (j0 + b < h.kk) word[b / 4] |= (static_cast<uint32_t>(values[static_cast<size_t>(o) * h.kk + j0 + b]) & 0xFFu) << (8 * (b % 4));
+        }
+        reinterpret_cast<uint4*>(h.packed)[(static_cast<size_t>(u) * chunks + c) * 32 + lane] = make_uint4(word[0], word[1], word[2], word[3]);
+    }
+}
+
+// values [c_out][kk] out of the expanded form.
+__global__ void __launch_bounds__(256) k_q8_values(const nm_q8_weights h, int8_t* __restrict__ values)
+{
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j >= h.kk) return;
+    for (int o = blockIdx.y; o < h.c_out; o += gridDim.y) {
+        const int c = h.indices[static_cast<size_t>(o / h.tile_t) * h.kk_ld + j], piece = c % 128 / 16;
+        values[static_cast<size_t>(o) * h.kk + j] = h.expanded[(static_cast<size_t>(c / 128) * h.rows + o) * 128 + ((piece ^ (o & 7)) << 4) + c % 16];
     }
 }
 
@@ -195,6 +222,7 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
     h->n_tiles = (c_out + tile_t - 1) / tile_t;
     h->k_blocks = (k + 127) / 128;
     h->rows = (c_out + 255) / 256 * 256;
+    if (packed_tile(*h) >= 8) h->units = (packed_tile(*h) + 7) / 8;
     size_t total = 0;
     auto place = [&total](size_t bytes) {
         const size_t here = total;
@@ -202,7 +230,8 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
         return here;
     };
     const size_t at_expanded = place(static_cast<size_t>(h->k_blocks) * h->rows * 128);
-    const size_t at_values = place(static_cast<size_t>(c_out) * h->kk_ld);
+    const size_t tiles = n_keep == m_group ? 1 : h->n_tiles;
+    const size_t at_packed = place(tiles * h->units * 8 * h->kk_ld);
     const size_t at_indices = place(static_cast<size_t>(h->n_tiles) * h->kk_ld * 2);
     const size_t at_scales = place(static_cast<size_t>(c_out) * 4);
     const size_t at_status = place(16);
@@ -212,7 +241,7 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
         return fail(NM_ERR_ALLOC, "%s: cannot allocate %zu bytes on the device", who, total);
     }
     h->expanded = reinterpret_cast<int8_t*>(h->block + at_expanded);
-    h->values = reinterpret_cast<int8_t*>(h->block + at_values);
+    h->packed = h->units ? reinterpret_cast<int8_t*>(h->block + at_packed) : nullptr;
     h->indices = reinterpret_cast<uint16_t*>(h->block + at_indices);
     h->scales = reinterpret_cast<float*>(h->block + at_scales);
     h->status = reinterpret_cast<int*>(h->block + at_status);
@@ -227,13 +256,20 @@ void discard(nm_q8_weights* h, bool idle)
     delete h;
 }
 
-// Layouts, and the one synchronisation: the handle is complete when the call returns, whatever stream uses it next.
-nm_status_t finish(const char* who, nm_q8_weights* h, const int8_t* values, const uint16_t* idx, int ld, cudaStream_t st)
+// Layouts from values [c_out][kk] and index rows (`idx` NULL: the handle has its own), and the one synchronisation: the handle is
+// complete when the call returns, whatever stream uses it next.
+nm_status_t finish(const char* who, nm_q8_weights* h, const int8_t* values, const uint16_t* idx, cudaStream_t st)
 {
     cudaError_t e = cudaMemsetAsync(h->status, 0, 16, st);
-    int* bad = h->status + 3;   // (cleared again below: zero stays)
-    k_q8_layout<<<dim3(h->k_blocks, h->rows / 64), 256, 0, st>>>(values, idx, ld, *h, bad);
-    nmhost::count_launch(1);
+    int* bad = h->status + 3;
+    if (idx) k_q8_indices<<<dim3((h->kk_ld + 255) / 256, h->n_tiles), 256, 0, st>>>(idx, *h, bad);
+    k_q8_expand<<<dim3(h->k_blocks, h->rows / 64), 256, 0, st>>>(values, *h);
+    nmhost::count_launch(idx ? 2 : 1);
+    if (h->packed) {
+        const int tile = packed_tile(*h), n_units = (h->c_out + tile - 1) / tile * h->units;
+        k_q8_pack<<<dim3((h->kk_ld / 64 + 7) / 8, std::min(n_units, 65535)), 256, 0, st>>>(values, *h, tile);
+        nmhost::count_launch(1);
+    }
     if (e == cudaSuccess) e = cudaGetLastError();
     int found = 0;
     if (e == cudaSuccess) e = cudaMemcpyAsync(&found, bad, sizeof(int), cudaMemcpyDeviceToHost, st);
@@ -289,21 +325,22 @@ nm_status_t nm_q8_prune(const float* w_dense, int c_out, int k, int n_keep, int 
     nm_q8_weights* h = nullptr;
     nm_status_t s = make("nm_q8_prune", c_out, k, n_keep, m_group, tile_t, &h);
     if (s != NM_OK) return s;
-    // scores (fp64) and keep flags of every (tile, column)
-    const size_t cells = static_cast<size_t>(h->n_tiles) * k;
+    // scores (fp64) and keep flags of every (tile, column), values
+    const size_t cells = static_cast<size_t>(h->n_tiles) * k, want = cells * 9 + static_cast<size_t>(c_out) * h->kk;
     size_t scratch_bytes = 0;
-    uint8_t* scratch = static_cast<uint8_t*>(nmhost::device_block_alloc(cells * 9, h->device, &scratch_bytes));
+    uint8_t* scratch = static_cast<uint8_t*>(nmhost::device_block_alloc(want, h->device, &scratch_bytes));
     if (!scratch) {
         discard(h, true);
-        return fail(NM_ERR_ALLOC, "nm_q8_prune: cannot allocate %zu bytes of scratch", cells * 9);
+        return fail(NM_ERR_ALLOC, "nm_q8_prune: cannot allocate %zu bytes of scratch", want);
     }
+    int8_t* values = reinterpret_cast<int8_t*>(scratch + cells * 9);
     cudaError_t e = cudaMemsetAsync(h->indices, 0, static_cast<size_t>(h->n_tiles) * h->kk_ld * 2, st);
     nmhost::select_columns(w_dense, c_out, k, h->kk, h->kk_ld, n_keep, m_group, tile_t, reinterpret_cast<double*>(scratch), scratch + cells * 8,
                            h->indices, st);
-    k_q8_quantise<<<c_out, 256, 0, st>>>(w_dense, k, h->kk, h->kk_ld, tile_t, h->indices, h->values, h->scales);
+    k_q8_quantise<<<c_out, 256, 0, st>>>(w_dense, k, h->kk, h->kk_ld, tile_t, h->indices, values, h->scales);
     nmhost::count_launch(1);
     if (e == cudaSuccess) e = cudaGetLastError();
-    s = e == cudaSuccess ? finish("nm_q8_prune", h, h->values, h->indices, h->kk_ld, st) : fail(NM_ERR_CUDA, "nm_q8_prune: %s", cudaGetErrorString(e));
+    s = e == cudaSuccess ? finish("nm_q8_prune", h, values, nullptr, st) : fail(NM_ERR_CUDA, "nm_q8_prune: %s", cudaGetErrorString(e));
     nmhost::device_block_free(scratch, scratch_bytes, h->device, s == NM_OK);
     if (s != NM_OK) {
         discard(h, false);
@@ -328,7 +365,7 @@ nm_status_t nm_q8_weights_import(const int8_t* values, const float* scales, cons
         return fail(NM_ERR_INVALID_ARG, "nm_q8_weights_import: values and indices must lie on the current device");
     }
     const cudaError_t e = cudaMemcpyAsync(h->scales, scales, static_cast<size_t>(c_out) * 4, cudaMemcpyDeviceToDevice, st);
-    s = e == cudaSuccess ? finish("nm_q8_weights_import", h, values, indices, h->kk, st) : fail(NM_ERR_CUDA, "nm_q8_weights_import: %s", cudaGetErrorString(e));
+    s = e == cudaSuccess ? finish("nm_q8_weights_import", h, values, indices, st) : fail(NM_ERR_CUDA, "nm_q8_weights_import: %s", cudaGetErrorString(e));
     if (s != NM_OK) {
         discard(h, false);
         return s;
@@ -342,7 +379,13 @@ nm_status_t nm_q8_weights_export(const nm_q8_weights_t* w, int8_t* values, float
     if (!valid(w)) return fail(NM_ERR_INVALID_ARG, "nm_q8_weights_export: bad weights handle");
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = cudaSuccess;
-    if (values) e = cudaMemcpy2DAsync(values, w->kk, w->values, w->kk_ld, w->kk, w->c_out, cudaMemcpyDeviceToDevice, st);
+    if (values) {
+        if (!nmhost::kernel_may_touch(values, w->expanded, w->device))
+            return fail(NM_ERR_INVALID_ARG, "nm_q8_weights_export: values must lie on the handle's device, which is the current one");
+        k_q8_values<<<dim3((w->kk + 255) / 256, std::min(w->c_out, 65535)), 256, 0, st>>>(*w, values);
+        nmhost::count_launch(1);
+        e = cudaGetLastError();
+    }
     if (e == cudaSuccess && scales) e = cudaMemcpyAsync(scales, w->scales, static_cast<size_t>(w->c_out) * 4, cudaMemcpyDeviceToDevice, st);
     if (e == cudaSuccess && indices)
         e = cudaMemcpy2DAsync(indices, w->kk * 2, w->indices, w->kk_ld * 2, w->kk * 2, w->n_tiles, cudaMemcpyDeviceToDevice, st);
@@ -412,6 +455,7 @@ nm_status_t nm_q8_linear(const nm_q8_weights_t* w, const int8_t* x, long long x_
     if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear: cudaGetDevice: %s", cudaGetErrorString(e));
     if (dev != w->device) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: the handle belongs to device %d, current is %d", w->device, dev);
     const Q8Linear p = {w, x, x_ld, x_scale, bias, y, y_ld, tokens, y_dtype};
+    if (nmhost::q8_few_takes(p)) return nmhost::launch_q8_few(p, static_cast<cudaStream_t>(cuda_stream));
     return nmhost::launch_q8_gemm(p, static_cast<cudaStream_t>(cuda_stream));
 }
 

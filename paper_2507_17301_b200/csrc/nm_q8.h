@@ -14,11 +14,13 @@ struct nm_q8_weights {
     uint8_t* block;        // the handle's device memory: one allocation that every array below lies in
     size_t block_bytes;
     int c_out, k, kk, n_keep, m_group, tile_t, n_tiles;
-    int kk_ld;             // row pitch of `values` and `indices`: kk rounded up to a multiple of 64 (zeros in between)
+    int kk_ld;             // row pitch of `indices`: kk rounded up to a multiple of 64 (column 0 in between)
     int k_blocks, rows;    // of `expanded`: ceil(k / 128) blocks, c_out rounded up to a multiple of 256
-    int8_t* values;        // [c_out][kk_ld]
+    int units;             // of `packed` in a tile (a dense layer is one tile): its rows in eights; 0: no packed form
     float* scales;         // [c_out]
     uint16_t* indices;     // [n_tiles][kk_ld]
+    int8_t* packed;        // [tile][unit][kk_ld / 64][8 rows x 4 quarters][16]: retained weights, zeros behind the last column and row; the 512
+                           // bytes of a unit and 64 columns are one warp's load, row and quarter by lane.  NULL for tiles of less than 8 rows
     int8_t* expanded;      // [k_blocks][rows][128]: pruned columns are zeros; a row's eight 16-byte pieces stand in the order of the
                            // tensor core's 128-byte swizzle (piece i of row r at i ^ (r & 7))
     int* status;           // device int[4], as in nm_weights
@@ -59,6 +61,10 @@ namespace nmhost {
 nm_status_t launch_q8_rows_f32(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
 nm_status_t launch_q8_rows_bf16(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
 nm_status_t launch_q8_rows_f16(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
+
+// nm_q8_few.cu: few tokens (32 at most); false where the kernel does not take the call
+bool q8_few_takes(const Q8Linear& p);
+nm_status_t launch_q8_few(const Q8Linear& p, cudaStream_t st);
 
 // nm_q8_gemm.cu
 nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st);
