@@ -562,6 +562,18 @@ __device__ __forceinline__ void umma_tf32_ss_pair(uint32_t d_tmem, uint64_t ades
         "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// The same on signed 8-bit integers (x 32 columns), sums in 32-bit integers.
+__device__ __forceinline__ void umma_s8_ss_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t"
+        "}\n" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 // Arrives on the barrier at offset `bar` in BOTH CTAs once every pair MMA issued so far has finished.
 __device__ __forceinline__ void umma_commit_pair(uint32_t bar)
 {

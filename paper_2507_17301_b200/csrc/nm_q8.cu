@@ -456,6 +456,7 @@ nm_status_t nm_q8_linear(const nm_q8_weights_t* w, const int8_t* x, long long x_
     if (dev != w->device) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: the handle belongs to device %d, current is %d", w->device, dev);
     const Q8Linear p = {w, x, x_ld, x_scale, bias, y, y_ld, tokens, y_dtype};
     if (nmhost::q8_few_takes(p)) return nmhost::launch_q8_few(p, static_cast<cudaStream_t>(cuda_stream));
+    if (nmhost::q8_pair_takes(p)) return nmhost::launch_q8_pair(p, static_cast<cudaStream_t>(cuda_stream));
     return nmhost::launch_q8_gemm(p, static_cast<cudaStream_t>(cuda_stream));
 }
 

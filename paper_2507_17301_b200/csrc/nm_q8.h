@@ -69,6 +69,13 @@ nm_status_t launch_q8_few(const Q8Linear& p, cudaStream_t st);
 // nm_q8_gemm.cu
 nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st);
 
+// nm_q8_pair.cu: many tokens
+bool q8_pair_takes(const Q8Linear& p);
+nm_status_t launch_q8_pair(const Q8Linear& p, cudaStream_t st);
+
+// Activations [tokens][x_ld] as a tiled tensor map with a 128-column x `rows` box, 128-byte swizzle.
+bool q8_encode_x(const Q8Linear& p, int rows, void* tensor_map);
+
 // nm_prune.cu: retained columns of every tile by their L1 norms; `score` and `keep`: scratch of n_tiles * k entries each
 void select_columns(const float* w_dense, int c_out, int k, int kk, int kk_ld, int n_keep, int m_group, int tile_t, double* score,
                     uint8_t* keep, uint16_t* indices, cudaStream_t st);

@@ -42,16 +42,42 @@ struct GemmArgs {
 };
 
 template <typename T>
-__device__ __forceinline__ void put(void* y, size_t at, float v);
+__device__ __forceinline__ T narrow(float v);
 template <>
-__device__ __forceinline__ void put<float>(void* y, size_t at, float v) { static_cast<float*>(y)[at] = v; }
+__device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <>
-__device__ __forceinline__ void put<__nv_bfloat16>(void* y, size_t at, float v) { static_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v); }
+__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <>
-__device__ __forceinline__ void put<__half>(void* y, size_t at, float v) { static_cast<__half*>(y)[at] = __float2half_rn(v); }
+__device__ __forceinline__ __half narrow<__half>(float v) { return __float2half_rn(v); }
 
 template <typename T>
-__global__ void __launch_bounds__(THREADS, 1) k_q8_gemm(const GemmArgs g, const __grid_constant__ CUtensorMap tm_x)
+struct alignas(4 * sizeof(T)) Four {
+    T v[4];
+};
+// Four channels of a token, the first `n` of which exist.
+template <typename T>
+__device__ __forceinline__ void put4(T* y, const float (&v)[4], int n, bool aligned)
+{
+    Four<T> f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = narrow<T>(v[i]);
+    if (aligned && n >= 4) {
+        *reinterpret_cast<Four<T>*>(y) = f;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < n) y[i] = f.v[i];
+}
+__device__ __forceinline__ int4 load_int4(uint32_t at)
+{
+    int4 v;
+    asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const __grid_constant__ CUtensorMap tm_x)
 {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t s_full[NSTAGE_MAX], s_free[NSTAGE_MAX], s_acc, s_recv;
@@ -138,58 +164,63 @@ __global__ void __launch_bounds__(THREADS, 1) k_q8_gemm(const GemmArgs g, const 
         pdl_wait();
         const int e = tid - 64;   // 0 to 127
         for (int i = e; i < g.bn; i += 128) s_scale[i] = t0 + i < g.tokens ? __ldg(g.x_scale + t0 + i) : 0.f;
-        const int q = warp & 3;
-        const int row = q * 32 + lane, ch = c0 + row;
-        const float ws = ch < g.c_out ? __ldg(g.w_scale + ch) : 0.f;
-        const float bias = g.bias && ch < g.c_out ? __ldg(g.bias + ch) : 0.f;
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        // a lane stores four channels of a token at a time (every fourth token is this warp's)
+        const int row = (warp & 3) * 32 + lane, ch = c0 + lane * 4, n_ch = g.c_out - ch;
+        float ws[4], bias[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ws[i] = i < n_ch ? __ldg(g.w_scale + ch + i) : 0.f;
+            bias[i] = g.bias && i < n_ch ? __ldg(g.bias + ch + i) : 0.f;
+        }
+        const bool aligned = g.y_ld % 4 == 0 && reinterpret_cast<uintptr_t>(g.y) % (4 * sizeof(T)) == 0;
         const bool ok = mbar_wait(smem_u32(&s_acc), 0);
         if (!ok) *abort_flag = 3;
         tc_fence_after();
-        const uint32_t mine = tmem + (static_cast<uint32_t>(q * 32) << 16);
-        if (g.ks == 1) {
-            for (int b = 0; b < g.bn; b += 16) {
-                uint32_t v[16];
-                tmem_ld16(mine + b, v);
-                tmem_ld_wait();
-                if (ok && ch < g.c_out) {
+        // sums by token into the ring, whose loads have all been used: a lane holds a channel of 32 tokens, a row of the ring is a token
+        const uint32_t mine = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        for (int b = 0; b < g.bn; b += 16) {
+            uint32_t v[16];
+            tmem_ld16(mine + b, v);
+            tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (t0 + b + i < g.tokens)
-                            put<T>(g.y, static_cast<size_t>(t0 + b + i) * g.y_ld + ch, fmaf(static_cast<float>(static_cast<int>(v[i])) * s_scale[b + i], ws, bias));
-                }
-            }
-        } else {
-            // partial sums by token into the ring, whose loads have all been used; then each CTA's run of tokens to that CTA
-            for (int b = 0; b < g.bn; b += 16) {
-                uint32_t v[16];
-                tmem_ld16(mine + b, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(ring + static_cast<uint32_t>((b + i) * 128 + row) * 4u), "r"(v[i]) : "memory");
-            }
+            for (int i = 0; i < 16; ++i)
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(ring + static_cast<uint32_t>((b + i) * 128 + row) * 4u), "r"(v[i]) : "memory");
+        }
+        const int run = g.bn / g.ks;   // tokens that this CTA finishes
+        uint32_t parts = ring;
+        bool complete = ok;
+        if (g.ks > 1) {
+            // each CTA's run of tokens to that CTA
             fence_proxy_async();
             asm volatile("bar.sync 1, 128;" ::: "memory");
-            const int run = g.bn / g.ks;
             if (e == 0) {
                 for (int d = 0; d < g.ks; ++d)
                     bulk_copy_cluster(mapa_shared(recv + rank * run * 512u, d), ring + static_cast<uint32_t>(d * run) * 512u, static_cast<uint32_t>(run) * 512u,
                                       mapa_shared(smem_u32(&s_recv), d));
             }
-            if (!mbar_wait_cluster(smem_u32(&s_recv), 0)) *abort_flag = 4;
-            else if (ch < g.c_out) {
-                for (int i = 0; i < run; ++i) {
-                    int sum = 0;
-                    for (int s = 0; s < g.ks; ++s) {
-                        int v;
-                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(recv + static_cast<uint32_t>((s * run + i) * 128 + row) * 4u) : "memory");
-                        sum += v;
-                    }
-                    const int at = static_cast<int>(rank) * run + i;
-                    if (t0 + at < g.tokens)
-                        put<T>(g.y, static_cast<size_t>(t0 + at) * g.y_ld + ch, fmaf(static_cast<float>(sum) * s_scale[at], ws, bias));
+            if (!mbar_wait_cluster(smem_u32(&s_recv), 0)) {
+                *abort_flag = 4;
+                complete = false;
+            }
+            parts = recv;
+        } else {
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+        }
+        if (complete) {
+            const int first = static_cast<int>(rank) * run;
+#pragma unroll 2
+            for (int i = warp - 2; i < run; i += 4) {
+                const int token = t0 + first + i;
+                if (token >= g.tokens) break;
+                int4 sum = load_int4(parts + static_cast<uint32_t>(i * 128 + lane * 4) * 4u);
+                for (int s = 1; s < g.ks; ++s) {
+                    const int4 v = load_int4(parts + static_cast<uint32_t>((s * run + i) * 128 + lane * 4) * 4u);
+                    sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
                 }
+                const float xs = s_scale[first + i];
+                const float v[4] = {fmaf(static_cast<float>(sum.x) * xs, ws[0], bias[0]), fmaf(static_cast<float>(sum.y) * xs, ws[1], bias[1]),
+                                    fmaf(static_cast<float>(sum.z) * xs, ws[2], bias[2]), fmaf(static_cast<float>(sum.w) * xs, ws[3], bias[3])};
+                put4<T>(static_cast<T*>(g.y) + static_cast<size_t>(token) * g.y_ld + ch, v, n_ch, aligned);
             }
         }
     }
@@ -209,6 +240,17 @@ __global__ void __launch_bounds__(THREADS, 1) k_q8_gemm(const GemmArgs g, const 
 
 namespace nmhost {
 
+bool q8_encode_x(const Q8Linear& p, int rows, void* tensor_map)
+{
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.w->k), static_cast<cuuint64_t>(p.tokens)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.x_ld)};
+    const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(rows)}, es[2] = {1, 1};
+    return nmtm::available() &&
+           nmtm::encoders().tiled(static_cast<CUtensorMap*>(tensor_map), CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(p.x), dims, strides, box, es,
+                                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
 {
     const nm_q8_weights* w = p.w;
@@ -216,28 +258,29 @@ nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
     g.expanded = w->expanded; g.w_scale = w->scales; g.x_scale = p.x_scale; g.bias = p.bias; g.y = p.y; g.y_ld = p.y_ld; g.status = w->status;
     g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows; g.k_blocks = w->k_blocks;
     g.c_tiles = (w->c_out + 127) / 128;
+    // The narrowest tiles that still are one round, us: 4096 -> 4096, 128 tokens in tiles of 16 / 32 / 64 / 128: 16.0 / 8.7 / 9.2 / 11.1; 512 tokens:
+    // 56 / 34 / 19 / 12.2.  A split of the reduction axis pays where half the SMs would idle (16 tokens, 2048 -> 2048: 5.0 whole, 3.8 in
+    // four), not in eight (7.9).
     g.bn = 16;
-    while (g.bn < 256 && g.bn < p.tokens) g.bn *= 2;
-    // far fewer tiles than SMs: narrower ones (a split has to hold a tile's partial sums beside the ring)
-    while (g.bn == 256 && 2ll * g.c_tiles * ((p.tokens + 255) / 256) <= sm_count()) g.bn = 128;
+    while (g.bn < 256 && g.bn < p.tokens && static_cast<long long>(g.c_tiles) * ((p.tokens + g.bn - 1) / g.bn) > sm_count()) g.bn *= 2;
     const long long items = static_cast<long long>(g.c_tiles) * ((p.tokens + g.bn - 1) / g.bn);
     if (items > (1ll << 27)) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: too many tiles");
     g.ks = 1;
-    while (g.bn <= 128 && g.ks < 8 && items * g.ks * 2 <= sm_count() && g.k_blocks >= g.ks * 4) g.ks *= 2;
+    while (g.bn <= 128 && g.ks < 4 && items * g.ks * 2 <= sm_count() && g.k_blocks >= g.ks * 4) g.ks *= 2;
+    // More than a round of CTAs: two on an SM, one sets up and loads while the other finishes (in one round the deeper ring is faster:
+    // 4096 -> 4096, 512 tokens 12.2 us against 16.9)
+    const bool half = g.bn <= 128 && items > sm_count();
     g.stage_bytes = A_BYTES + g.bn * 128;
-    const int budget = 227 * 1024 - 1024 - 2048 - (g.ks > 1 ? g.bn * 512 : 0);
+    const int budget = (half ? 112 : 224) * 1024 - 1024 - 2048 - (g.ks > 1 ? g.bn * 512 : 0);
     g.stages = std::min(NSTAGE_MAX, budget / g.stage_bytes);
-    // (a split's partial sums, at most 64 KB, go through the ring, which has at least 144 KB then)
-    CUtensorMap tm;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(w->k), static_cast<cuuint64_t>(p.tokens)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.x_ld)};
-    const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(g.bn)}, es[2] = {1, 1};
-    if (!nmtm::available() ||
-        nmtm::encoders().tiled(&tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(p.x), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return fail(NM_ERR_CUDA, "nm_q8_linear: tensor-map encoding failed");
+    // (the sums of a tile, bn * 512 bytes, go through the ring, which has at least 96 KB, 192 KB with bn = 256)
+    alignas(64) CUtensorMap tm;
+    if (!q8_encode_x(p, g.bn, &tm)) return fail(NM_ERR_CUDA, "nm_q8_linear: tensor-map encoding failed");
     size_t smem = 1024 + static_cast<size_t>(g.stages) * g.stage_bytes + (g.ks > 1 ? g.bn * 512 : 0);
-    if (smem < NM_EXCLUSIVE_SMEM) smem = NM_EXCLUSIVE_SMEM;   // alone on its SM: CTAs of a cluster wait for each other while they hold tensor memory
+    // Alone on its SM: CTAs of a cluster wait for each other while they hold tensor memory.  The others need more than what the kernels
+    // that take all of it leave free.
+    if (!half && smem < NM_EXCLUSIVE_SMEM) smem = NM_EXCLUSIVE_SMEM;
+    if (half && smem < 76 * 1024) smem = 76 * 1024;   // (at most two on an SM, of 256 columns of tensor memory at most)
     void (*kernel)(GemmArgs, CUtensorMap) = p.y_type == NM_F32 ? k_q8_gemm<float> : p.y_type == NM_BF16 ? k_q8_gemm<__nv_bfloat16> : k_q8_gemm<__half>;
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear: cudaFuncSetAttribute: %s", cudaGetErrorString(e));
