@@ -4,7 +4,7 @@
 //   a = max |p_j|,   q_j = nearest integer to 127 p_j / a (ties to even),   scale = a / 127, times 1 / sqrt(mean s^2 + eps) for rmsnorm
 //
 // The norm's factor cancels out of q, so one reduction over the row gives both the sum of squares and the maximum, and a row is
-// read once: its p stay in registers (rows of more than 16384 columns are read again, out of the L2).
+// read once: its p stay in registers (rows of more than 32768 columns, 16384 of 32 bits, are read again, out of the L2).
 //
 // q is the integer that exact arithmetic gives, whatever the kernel's shape: p is worked out in 32 bits, and where 127 p / a lies so
 // near a border between two integers that their error could decide, it is worked out again in 64; the maximum is taken in 64
@@ -146,26 +146,30 @@ __device__ __forceinline__ Pair two_of(const Eight<T>& e, int i)
     }
 }
 
-// Relative error of p times 127 / a in 32 bits, with room: four roundings (2.4e-7); for silu_mul the exponent's two
-// roundings of up to 115 * 2^-24 each (9.5e-6 in all, g >= -80), 2^-22 and 2^-23 of the exponential and the reciprocal, and
-// four roundings.
+// Relative error of p times 127 / a in 32 bits, with room: five roundings (3e-7); for silu_mul beside them the exponent's two
+// roundings of up to 126 * 2^-24 each (1.04e-5 in all, g >= -87), 2^-22 and 2^-23 of the exponential and the reciprocal, and three more.
 template <Q8RowOp OP>
 constexpr float kError = OP == Q8_SILU_MUL ? 1.5e-5f : 4e-7f;
-// silu_mul beyond g = -80: less than kMostProduct * 2^-115 * 80, of which the bound on the row's maximum makes less than 2^-8 of kBorder
+// silu_mul beyond g = -87: less than kMostProduct * 2^-125 * 88, which is nothing beside kLeastTop
 constexpr float kMostProduct = 0x1p20f, kLeastTop = 0x1p-60f;
 constexpr float kMostTop = 0x1p100f;   // (127 p and 1 / a stay normal numbers)
+constexpr float kMostSum = 0x1p120f;
 // How near 127 p / a may come to a border between two integers, beside its own error, before 64 bits decide.
 constexpr float kBorder = 0.5f - 1e-7f;
 
 // The products g u and g u / (1 + exp(-g)): (g u) first, whose underflow cannot matter beside kLeastTop.  Where the exponential
-// or its reciprocal leaves 32 bits (g < -87) the result is 0.
+// or its reciprocal leaves 32 bits (g < -87) the result is 0.  (Making good the exponent's rounding leaves a twentieth of the quotients
+// to 64 bits and costs more than it saves: 4096 x 12288 bf16 72 us instead of 69.)
 __device__ __forceinline__ void gated(Pair g, Pair u, Pair* product, Pair* p)
 {
     float a, b;
-    split(mul2(g, pair(-1.44269504f, -1.44269504f)), a, b);
+    split(g, a, b);
+    a *= -1.44269504f;
+    b *= -1.44269504f;
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
-    split(add2(pair(a, b), pair(1.f, 1.f)), a, b);
+    a += 1.f;
+    b += 1.f;
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
     *product = mul2(g, u);
@@ -213,11 +217,12 @@ __device__ __forceinline__ bool product_of_non_zeros(const Q8Rows& a, size_t row
 
 constexpr float kRound = 12582912.f;   // adding 1.5 * 2^23 rounds to an integer, whose low byte is then the sum's
 
-// Distance of p * inv to the nearest integer plus what its error may add.
+// Distance of p * inv to the nearest integer plus what its error may add; the low byte of *k is the integer's.
 template <Q8RowOp OP>
-__device__ __forceinline__ float border_of(float p, float inv)
+__device__ __forceinline__ float border_of(float p, float inv, uint32_t* k)
 {
-    const float whole = fmaf(p, inv, kRound) - kRound;
+    const float n = fmaf(p, inv, kRound), whole = n - kRound;
+    *k = __float_as_uint(n);
     return fmaf(fabsf(whole), kError<OP>, fabsf(fmaf(p, inv, -whole)));
 }
 // One column's integer, which 32 bits left open, in 64 bits; top = 0: |p| itself instead.  x_at, r_at: where the column's inputs
@@ -345,7 +350,8 @@ __device__ __noinline__ void row_in_64(const Q8Rows& a, size_t row, int t, bool 
 
 // TPR threads take a row, each NV groups of eight columns, in steps of TPR groups.  KEEP: the row's p stay in registers (8 * NV * TPR >= h).
 // (at least 768 threads an SM)
-template <Q8RowOp OP, typename T, typename W, int TPR, int NV, bool KEEP, bool VEC>
+// TWO: two tensors are read (silu_mul, rmsnorm with a residual).  SLOTS: rows in shared memory at a time (0: none, straight to registers).
+template <Q8RowOp OP, bool TWO, typename T, typename W, int TPR, int NV, bool KEEP, bool VEC, int SLOTS>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 768 ? 1 : 768 / TPR) k_q8_rows(const __grid_constant__ Q8Rows a)
 {
     constexpr int ROWS = TPR < 128 ? 128 / TPR : 1;
@@ -355,7 +361,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     // p of at most 16 bits: 127 p is exact in 32, and 127 p / a is a half or further from it than fp32's half a place: 254 p - (2k + 1) a
     // is a multiple of p's last place, more than 2^-16 p, and that over 2 a is more than 2^-24 of the quotient
     constexpr bool DIVIDE = sizeof(T) == 2 && (OP == Q8_ROWS || (OP == Q8_RMSNORM && std::is_same_v<T, __nv_bfloat16> && sizeof(W) == 2));
-    constexpr bool ASYNC = KEEP && VEC;
+    constexpr bool ASYNC = SLOTS > 0;
+    static_assert(!ASYNC || (KEEP && VEC), "copied pieces are read once, 16 bytes at a time");
     extern __shared__ uint4 smem[];
     __shared__ Scratch scratch[2];   // rows take turns: a row's is written after the barrier behind the last reading of it
     const int t = threadIdx.x % TPR;
@@ -364,12 +371,11 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     nmk::pdl_launch_dependents();
     nmk::pdl_wait();
     // ASYNC: a thread copies its part of the next row into places of its own in shared memory while this row is reduced and written
-    // (no barrier, no registers; two sets of places taken in turn)
+    // (no barrier, no registers; two sets of places taken in turn, one where a row is too long for two)
     constexpr int PIECES = sizeof(T) / 2, THREADS = TPR < 128 ? 128 : TPR;
-    const bool two = OP == Q8_SILU_MUL || (OP == Q8_RMSNORM && a.r != nullptr);
-    const uint32_t places = nmk::smem_u32(smem) + threadIdx.x * 16u;
+    uint4* const places = smem + threadIdx.x;
     auto place = [&](int turn, int tensor, int i, int piece) {
-        return places + static_cast<uint32_t>((((turn * (two ? 2 : 1) + tensor) * NV + i) * PIECES + piece) * THREADS) * 16u;
+        return places + (((SLOTS == 2 ? turn : 0) * (TWO ? 2 : 1) + tensor) * NV * PIECES + i * PIECES + piece) * THREADS;
     };
     auto fetch = [&](size_t row, int turn) {
         const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
@@ -384,8 +390,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
                 const int bytes = (a.h - v * 8) * static_cast<int>(sizeof(T)) - piece * 16;
                 const uint32_t some = bytes < 16 ? (bytes > 0 ? bytes : 0) : 16;
                 const int from = some ? v * 8 + piece * (16 / static_cast<int>(sizeof(T))) : 0;
-                nmk::cp_async16(place(turn, 0, i, piece), x + from, some);
-                if (two) nmk::cp_async16(place(turn, 1, i, piece), r + from, some);
+                nmk::cp_async16(nmk::smem_u32(place(turn, 0, i, piece)), x + from, some);
+                if (TWO) nmk::cp_async16(nmk::smem_u32(place(turn, 1, i, piece)), r + from, some);
             }
         }
     };
@@ -393,15 +399,13 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         Eight<T> e;
 #pragma unroll
         for (int piece = 0; piece < PIECES; ++piece) {
-            uint4 u;
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(turn, tensor, i, piece)) : "memory");
-            reinterpret_cast<uint4*>(&e)[piece] = u;
+            reinterpret_cast<uint4*>(&e)[piece] = *place(turn, tensor, i, piece);
         }
         return e;
     };
     // (whole rows leave: ROWS > 1 has no barrier across warps)
     size_t row = static_cast<size_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
-    if constexpr (ASYNC) {
+    if constexpr (SLOTS == 2) {
         if (row < tokens) fetch(row, 0);
         nmk::cp_async_commit();
     }
@@ -410,8 +414,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     for (int turn = 0; row < tokens; row += step, turn ^= 1) {
     Scratch* sc = scratch + turn;
     const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
-    const T* r = a.r ? static_cast<const T*>(a.r) + row * a.r_ld : nullptr;
-    T* s_row = a.s ? static_cast<T*>(a.s) + row * a.s_ld : nullptr;
+    const T* r = TWO ? static_cast<const T*>(a.r) + row * a.r_ld : nullptr;
+    T* s_row = OP == Q8_RMSNORM && TWO ? static_cast<T*>(a.s) + row * a.s_ld : nullptr;
 
     Pair p[KEEP ? NV : 1][4];
     Pair sum2 = 0;
@@ -420,7 +424,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     auto values = [&](int v, Pair (&out)[4], const Eight<T>& ex, const Eight<T>& er, const Eight<W>& ew, bool first) {
         if constexpr (OP == Q8_RMSNORM) {
             Eight<T> es = ex;
-            if (two && first) {
+            if (TWO && first) {
                 es = add8<T>(ex, er);
                 store8<T, VEC>(s_row + v * 8, es, a.h - v * 8);
             }
@@ -461,9 +465,9 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             const int v = base + i * TPR, n = a.h - v * 8;
             if (n <= 0) continue;
             // the second reading of a norm's row finds the sum in memory
-            const T* from = OP == Q8_RMSNORM && r && !first ? s_row : x;
+            const T* from = OP == Q8_RMSNORM && TWO && !first ? s_row : x;
             ex[i] = load8<T, VEC>(from + v * 8, n);
-            if (OP == Q8_SILU_MUL || (OP == Q8_RMSNORM && r && first)) er[i] = load8<T, VEC>(r + v * 8, n);
+            if (TWO && (OP == Q8_SILU_MUL || first)) er[i] = load8<T, VEC>(r + v * 8, n);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -477,9 +481,13 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         }
     };
     if constexpr (ASYNC) {
-        if (row + step < tokens) fetch(row + step, turn ^ 1);
+        if constexpr (SLOTS == 2) {
+            if (row + step < tokens) fetch(row + step, turn ^ 1);
+        } else {
+            fetch(row, 0);
+        }
         nmk::cp_async_commit();
-        nmk::cp_async_wait<1>();
+        nmk::cp_async_wait<SLOTS - 1>();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = t + i * TPR;
@@ -487,7 +495,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             Eight<W> ew = {};
             if (v * 8 >= a.h) continue;
             if (OP == Q8_RMSNORM) ew = load8<W, VEC>(weight + v * 8, a.h - v * 8);   // (out of the L1: every row reads them)
-            if (two) er = fetched(turn, 1, i);
+            if (TWO) er = fetched(turn, 1, i);
             values(v, p[i], fetched(turn, 0, i), er, ew, true);
         }
     } else if constexpr (KEEP) {
@@ -505,6 +513,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         split(sum2, lo, hi);
         sum = lo + hi;
         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+        if (!(sum <= kMostSum)) top = NAN;   // (the row goes to 64 bits; 32 sums below the bound do not overflow)
     }
     // as bits: NaN above infinity above numbers
     uint32_t top_bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top) & 0x7FFFFFFFu);
@@ -516,14 +525,14 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         __syncthreads();
         const int lane = t & 31;
         top_bits = __reduce_max_sync(0xFFFFFFFFu, lane < TPR / 32 ? sc->top[lane] : 0u);
-        if constexpr (OP == Q8_RMSNORM) {
+        if (OP == Q8_RMSNORM && t < 32) {   // (only the first thread wants it)
             sum = lane < TPR / 32 ? sc->sum[lane] : 0.f;
             for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
         }
     }
     const float a32 = __uint_as_float(top_bits);
     // kLeastTop: what 32 bits lose below 2^-126 is then less than a step by far
-    if (!(a32 >= kLeastTop && a32 <= kMostTop && sum < INFINITY)) {
+    if (!(a32 >= kLeastTop && a32 <= kMostTop)) {
         // (after the others: a call in here would cost the loop registers)
         set_aside = true;
         if (t == 0) a.scale[row] = a32 == 0.f ? -2.f : -1.f;
@@ -531,7 +540,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     }
     // (element `at` of this thread's part: group at / 8, column at % 8 of it)
     auto input_at = [&](int tensor, int at) {
-        return ASYNC ? place(turn, two ? tensor : 0, at / 8, at % 8 / (8 / PIECES)) + static_cast<uint32_t>(at % (8 / PIECES) * sizeof(T)) : 0u;
+        return ASYNC ? nmk::smem_u32(place(turn, TWO ? tensor : 0, at / 8, at % 8 / (8 / PIECES))) + static_cast<uint32_t>(at % (8 / PIECES) * sizeof(T)) : 0u;
     };
     double a64 = a32;
     if constexpr (!EXACT) {
@@ -564,9 +573,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         if constexpr (OP == Q8_RMSNORM) scale *= 1.f / sqrtf(sum / static_cast<float>(a.h) + a.eps);
         a.scale[row] = scale < INFINITY ? scale : NAN;
     }
-    const float inv = 127.f / static_cast<float>(a64);
+    const float a32_top = static_cast<float>(a64), rcp = __frcp_rn(a32_top), inv = 127.f * rcp;
     int8_t* q_row = a.q + row * a.q_ld;
-    const float a32_top = static_cast<float>(a64);
     // q of the group `v`; a bit for each that 64 bits have to decide
     auto quantise = [&](int v, Pair (&f)[4]) {
         uint32_t k[8];
@@ -574,30 +582,23 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         if constexpr (DIVIDE) {
             // 127 p / a, rounded correctly (Markstein: a quotient from the reciprocal, its remainder by fma, one correction), and
             // that to an integer: a quotient between two halves keeps its side, a tie is exact (see DIVIDE)
-            const float rcp = 1.f / a32_top;
             const Pair r = pair(rcp, rcp), minus_a = pair(-a32_top, -a32_top);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Pair t = mul2(f[i], pair(127.f, 127.f)), y = mul2(t, r);
-                const Pair n = add2(fma2(fma2(y, minus_a, t), r, y), pair(kRound, kRound));
                 float lo, hi;
-                split(n, lo, hi);
-                k[2 * i] = __float_as_uint(lo);
-                k[2 * i + 1] = __float_as_uint(hi);
+                split(f[i], lo, hi);
+                const Pair t = pair(127.f * lo, 127.f * hi), y = mul2(t, r);
+                split(fma2(fma2(y, minus_a, t), r, y), lo, hi);
+                k[2 * i] = __float_as_uint(lo + kRound);
+                k[2 * i + 1] = __float_as_uint(hi + kRound);
             }
         } else {
-            // n = the nearest integer to p * inv, and how far off that is: within the error bound of a half, 64 bits decide
-            const Pair by = pair(inv, inv);
+            // the nearest integer to p * inv, and how far off that is: within the error bound of a half, 64 bits decide
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const Pair n = fma2(f[i], by, pair(kRound, kRound)), minus = fma2(n, pair(-1.f, -1.f), pair(kRound, kRound)), off = fma2(f[i], by, minus);
-                float n0, n1, m0, m1, d0, d1;
-                split(n, n0, n1);
-                split(minus, m0, m1);
-                split(off, d0, d1);
-                k[2 * i] = __float_as_uint(n0);
-                k[2 * i + 1] = __float_as_uint(n1);
-                border = top3(border, fmaf(fabsf(m0), kError<OP>, fabsf(d0)), fmaf(fabsf(m1), kError<OP>, fabsf(d1)));
+                float lo, hi;
+                split(f[i], lo, hi);
+                border = top3(border, border_of<OP>(lo, inv, &k[2 * i]), border_of<OP>(hi, inv, &k[2 * i + 1]));
             }
         }
         const uint32_t lo = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
@@ -608,7 +609,10 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         } else {
             for (int e = 0; e < n; ++e) q_row[v * 8 + e] = static_cast<int8_t>((e < 4 ? lo >> (8 * e) : hi >> (8 * (e - 4))) & 0xFFu);
         }
-        return border > kBorder ? which(f, [&](float p) { return border_of<OP>(p, inv) > kBorder; }) : 0u;
+        return border > kBorder ? which(f, [&](float p) {
+            uint32_t unused;
+            return border_of<OP>(p, inv, &unused) > kBorder;
+        }) : 0u;
     };
     auto decide = [&](uint32_t bits, int v0) {
         for (; bits; bits &= bits - 1u) {
@@ -641,60 +645,64 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     }
 }
 
-template <Q8RowOp OP, typename T, typename W, int TPR, int NV, bool KEEP, bool VEC>
+template <Q8RowOp OP, bool TWO, typename T, typename W, int TPR, int NV, bool KEEP, bool VEC, int SLOTS>
 cudaError_t launch_one(const Q8Rows& a, cudaStream_t st)
 {
     constexpr int rows = TPR < 128 ? 128 / TPR : 1, threads = TPR < 128 ? 128 : TPR;
     const int blocks = (a.tokens + rows - 1) / rows;
-    // two rows' places of each thread, of one or two tensors; as many blocks as an SM holds for certain (768 threads, 227 KB)
-    const size_t smem = KEEP && VEC ? static_cast<size_t>(threads) * NV * 8 * sizeof(T) * 2 * (a.r ? 2 : 1) : 0;
+    // as many blocks as an SM holds for certain (768 threads, 227 KB)
+    constexpr size_t smem = static_cast<size_t>(threads) * NV * 8 * sizeof(T) * SLOTS * (TWO ? 2 : 1);
     int resident = threads > 768 ? 1 : 768 / threads;
     if (smem && 225 * 1024 / (smem + 3072) < static_cast<size_t>(resident)) resident = static_cast<int>(225 * 1024 / (smem + 3072));
     resident *= nmhost::sm_count();
-    auto kernel = k_q8_rows<OP, T, W, TPR, NV, KEEP, VEC>;
+    auto kernel = k_q8_rows<OP, TWO, T, W, TPR, NV, KEEP, VEC, SLOTS>;
     const cudaError_t e = nmhost::ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
     return nmhost::launch_pdl(kernel, static_cast<unsigned>(blocks < resident ? blocks : resident), static_cast<unsigned>(threads), smem, st, a);
 }
 
-// Threads for a row: two groups of eight columns each, one where there are too few rows to fill the GPU.
-template <Q8RowOp OP, typename T, typename W>
+// Threads for a row, four groups of eight columns each (two of 32-bit numbers); fewer groups where there are too few rows to fill the GPU.
+template <Q8RowOp OP, bool TWO, typename T, typename W>
 cudaError_t launch_shape(const Q8Rows& a, bool vec, cudaStream_t st)
 {
+#define NM_ROWS(TPR, NV, KEEP, VEC, SLOTS) launch_one<OP, TWO, T, W, TPR, NV, KEEP, VEC, SLOTS>(a, st)
     if (!vec) {
-        if (a.h <= 512) return launch_one<OP, T, W, 32, 2, true, false>(a, st);
-        if (a.h <= 4096) return launch_one<OP, T, W, 256, 2, true, false>(a, st);
-        return launch_one<OP, T, W, 512, 2, false, false>(a, st);
+        if (a.h <= 512) return NM_ROWS(32, 2, true, false, 0);
+        if (a.h <= 4096) return NM_ROWS(256, 2, true, false, 0);
+        return NM_ROWS(512, 2, false, false, 0);
     }
     const bool few = a.tokens <= 2 * nmhost::sm_count();
-    if (a.h <= 512) return launch_one<OP, T, W, 32, 2, true, true>(a, st);
-    if (a.h <= 2048 && !few) return launch_one<OP, T, W, 128, 2, true, true>(a, st);
+    if (a.h <= 512) return NM_ROWS(32, 2, true, true, 2);
+    if (a.h <= 2048 && !few) return NM_ROWS(128, 2, true, true, 2);
     if (few) {
-        if (a.h <= 4096) return launch_one<OP, T, W, 512, 1, true, true>(a, st);
-        if (a.h <= 8192) return launch_one<OP, T, W, 1024, 1, true, true>(a, st);
+        if (a.h <= 4096) return NM_ROWS(512, 1, true, true, 2);
+        if (a.h <= 8192) return NM_ROWS(1024, 1, true, true, 2);
     }
-    // (32-bit numbers: half as many in the same places, and 16384 columns of two tensors would not fit)
     if constexpr (sizeof(T) == 4) {
-        if (a.h <= 4096) return launch_one<OP, T, W, 256, 2, true, true>(a, st);
-        if (a.h <= 8192) return launch_one<OP, T, W, 512, 2, true, true>(a, st);
+        if (a.h <= 4096) return NM_ROWS(256, 2, true, true, 2);
+        if (a.h <= 8192) return NM_ROWS(512, 2, true, true, 2);
+        if (a.h <= 16384) return NM_ROWS(1024, 2, true, true, 1);
     } else {
-        if (few && a.h <= 16384) return launch_one<OP, T, W, 1024, 2, true, true>(a, st);
-        if (a.h <= 4096) return launch_one<OP, T, W, 128, 4, true, true>(a, st);
-        if (a.h <= 8192) return launch_one<OP, T, W, 256, 4, true, true>(a, st);
-        if (a.h <= 12288) return launch_one<OP, T, W, 384, 4, true, true>(a, st);
-        if (a.h <= 16384) return launch_one<OP, T, W, 512, 4, true, true>(a, st);
+        if (few && a.h <= 16384) return NM_ROWS(1024, 2, true, true, 2);
+        if (a.h <= 4096) return NM_ROWS(128, 4, true, true, 2);
+        if (a.h <= 8192) return NM_ROWS(256, 4, true, true, 2);
+        if (a.h <= 12288) return NM_ROWS(384, 4, true, true, 2);
+        if (a.h <= 16384) return NM_ROWS(512, 4, true, true, 2);
+        if (a.h <= 32768) return NM_ROWS(1024, 4, true, true, 1);
     }
-    return launch_one<OP, T, W, 512, 2, false, true>(a, st);
+    return NM_ROWS(512, 2, false, true, 0);
+#undef NM_ROWS
 }
 
 template <typename T>
 nm_status_t launch(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st)
 {
     cudaError_t e;
-    if (op == Q8_SILU_MUL) e = launch_shape<Q8_SILU_MUL, T, T>(a, vec, st);
-    else if (op == Q8_ROWS) e = launch_shape<Q8_ROWS, T, T>(a, vec, st);
-    else if (sizeof(T) == 2 && weight_type == NM_F32) e = launch_shape<Q8_RMSNORM, T, float>(a, vec, st);
-    else e = launch_shape<Q8_RMSNORM, T, T>(a, vec, st);
+    const bool wide = sizeof(T) == 2 && weight_type == NM_F32;
+    if (op == Q8_SILU_MUL) e = launch_shape<Q8_SILU_MUL, true, T, T>(a, vec, st);
+    else if (op == Q8_ROWS) e = launch_shape<Q8_ROWS, false, T, T>(a, vec, st);
+    else if (a.r) e = wide ? launch_shape<Q8_RMSNORM, true, T, float>(a, vec, st) : launch_shape<Q8_RMSNORM, true, T, T>(a, vec, st);
+    else e = wide ? launch_shape<Q8_RMSNORM, false, T, float>(a, vec, st) : launch_shape<Q8_RMSNORM, false, T, T>(a, vec, st);
     nmhost::count_launch(1);
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) return nmhost::fail(NM_ERR_CUDA, "8-bit row kernel launch: %s", cudaGetErrorString(e));
