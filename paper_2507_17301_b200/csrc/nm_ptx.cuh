@@ -444,6 +444,7 @@ __host__ __device__ constexpr uint32_t umma_idesc_s8(int m, int n)
            | (static_cast<uint32_t>(n >> 3) << 17)    // N / 8
            | (static_cast<uint32_t>(m >> 4) << 24);   // M / 16
 }
+constexpr uint32_t kSparseA = 1u << 2;   // bit of an instruction descriptor
 __device__ __forceinline__ void umma_s8_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
@@ -573,6 +574,24 @@ __device__ __forceinline__ void umma_s8_ss_pair(uint32_t d_tmem, uint64_t adesc,
         "}\n" ::"r"(d_tmem),
         "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
+}
+// The same with a sparse A (x 64 columns): of four adjacent columns two are in shared memory, and tensor memory says which, two bits
+// each, in 32-bit words of eight fours: lane = row, the two words of the 64 columns in two columns from `meta` on.
+__device__ __forceinline__ void umma_s8_sparse_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t meta, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.sp.cta_group::2.kind::i8 [%0], %1, %2, [%3], %4, p;\n\t"
+        "}\n" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(meta), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// tmem_cp_128x256b from each CTA's shared memory to its own tensor memory, issued by the first CTA.
+__device__ __forceinline__ void tmem_cp_128x256b_pair(uint32_t taddr, uint64_t sdesc)
+{
+    asm volatile("tcgen05.cp.cta_group::2.128x256b [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
 // Arrives on the barrier at offset `bar` in BOTH CTAs once every pair MMA issued so far has finished.
 __device__ __forceinline__ void umma_commit_pair(uint32_t bar)

@@ -168,6 +168,55 @@ __global__ void __launch_bounds__(256) k_q8_expand(const int8_t* __restrict__ va
     }
 }
 
+// Sparse form out of the expanded one: a thread takes 32 columns of a row, 16 bytes and a word of places.  Of four columns the two
+// that are not zero, or as many as there are and the first others.
+__global__ void __launch_bounds__(256) k_q8_sparse(const nm_q8_weights h)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x, r = i / 8, eighth = i % 8, sb = blockIdx.y;
+    if (r >= h.rows) return;
+    uint32_t in[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u}, out[4] = {0u, 0u, 0u, 0u}, places = 0u;
+    const int kb = sb * 2 + eighth / 4;
+    if (kb < h.k_blocks) {
+        const uint8_t* row = reinterpret_cast<const uint8_t*>(h.expanded) + (static_cast<size_t>(kb) * h.rows + r) * 128;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const uint4 u = *reinterpret_cast<const uint4*>(row + (((eighth % 4 * 2 + p) ^ (r & 7)) << 4));
+            in[p * 4] = u.x; in[p * 4 + 1] = u.y; in[p * 4 + 2] = u.z; in[p * 4 + 3] = u.w;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        uint32_t set = 0u;   // columns that are not zero
+        for (int b = 0; b < 4; ++b)
+            if (in[q] >> (8 * b) & 0xFFu) set |= 1u << b;
+        for (int b = 0; b < 4 && __popc(set) < 2; ++b) set |= 1u << b;
+        const int first = __ffs(set) - 1, second = __ffs(set & (set - 1u)) - 1;
+        places |= static_cast<uint32_t>(first | second << 2) << (4 * q);
+        const uint32_t two = (in[q] >> (8 * first) & 0xFFu) | (in[q] >> (8 * second) & 0xFFu) << 8;
+        out[q / 2] |= two << (16 * (q % 2));
+    }
+    uint8_t* dst = reinterpret_cast<uint8_t*>(h.sparse) + (static_cast<size_t>(sb) * h.rows + r) * 128;
+    *reinterpret_cast<uint4*>(dst + ((eighth ^ (r & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
+    uint8_t* to = h.places + (static_cast<size_t>(sb) * (h.rows / 128) + r / 128) * 4096;
+    *reinterpret_cast<uint32_t*>(to + r % 128 / 8 * 256 + eighth / 4 * 128 + r % 8 * 16 + eighth % 4 * 4) = places;
+}
+
+// Most columns that an N:M pattern can keep of four aligned ones.
+int most_of_four(int n_keep, int m_group)
+{
+    int most = 0;
+    for (int i = 0; i < m_group; ++i) {   // (the pattern repeats after m_group fours)
+        int kept = 0;
+        for (int c = 4 * i, end = 4 * i + 4; c < end;) {
+            const int stop = std::min(end, (c / m_group + 1) * m_group);
+            kept += std::min(n_keep, stop - c);
+            c = stop;
+        }
+        most = std::max(most, kept);
+    }
+    return most;
+}
+
 int packed_tile(const nm_q8_weights& h) { return h.n_keep == h.m_group ? h.c_out : h.tile_t; }
 
 // Packed form from values [c_out][kk]: a warp writes a unit's 512 bytes of 64 columns.
@@ -222,6 +271,7 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
     h->n_tiles = (c_out + tile_t - 1) / tile_t;
     h->k_blocks = (k + 127) / 128;
     h->rows = (c_out + 255) / 256 * 256;
+    if (most_of_four(n_keep, m_group) <= 2) h->s_blocks = (k + 255) / 256;
     if (packed_tile(*h) >= 8) h->units = (packed_tile(*h) + 7) / 8;
     size_t total = 0;
     auto place = [&total](size_t bytes) {
@@ -232,6 +282,7 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
     const size_t at_expanded = place(static_cast<size_t>(h->k_blocks) * h->rows * 128);
     const size_t tiles = n_keep == m_group ? 1 : h->n_tiles;
     const size_t at_packed = place(tiles * h->units * 8 * h->kk_ld);
+    const size_t at_sparse = place(static_cast<size_t>(h->s_blocks) * h->rows * 128), at_places = place(static_cast<size_t>(h->s_blocks) * h->rows * 32);
     const size_t at_indices = place(static_cast<size_t>(h->n_tiles) * h->kk_ld * 2);
     const size_t at_scales = place(static_cast<size_t>(c_out) * 4);
     const size_t at_status = place(16);
@@ -243,6 +294,10 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
     h->expanded = reinterpret_cast<int8_t*>(h->block + at_expanded);
     h->packed = h->units ? reinterpret_cast<int8_t*>(h->block + at_packed) : nullptr;
     h->indices = reinterpret_cast<uint16_t*>(h->block + at_indices);
+    if (h->s_blocks) {
+        h->sparse = reinterpret_cast<int8_t*>(h->block + at_sparse);
+        h->places = h->block + at_places;
+    }
     h->scales = reinterpret_cast<float*>(h->block + at_scales);
     h->status = reinterpret_cast<int*>(h->block + at_status);
     *out = h;
@@ -268,6 +323,10 @@ nm_status_t finish(const char* who, nm_q8_weights* h, const int8_t* values, cons
     if (h->packed) {
         const int tile = packed_tile(*h), n_units = (h->c_out + tile - 1) / tile * h->units;
         k_q8_pack<<<dim3((h->kk_ld / 64 + 7) / 8, std::min(n_units, 65535)), 256, 0, st>>>(values, *h, tile);
+        nmhost::count_launch(1);
+    }
+    if (h->sparse) {
+        k_q8_sparse<<<dim3(h->rows / 32, h->s_blocks), 256, 0, st>>>(*h);
         nmhost::count_launch(1);
     }
     if (e == cudaSuccess) e = cudaGetLastError();

@@ -17,12 +17,16 @@ struct nm_q8_weights {
     int kk_ld;             // row pitch of `indices`: kk rounded up to a multiple of 64 (column 0 in between)
     int k_blocks, rows;    // of `expanded`: ceil(k / 128) blocks, c_out rounded up to a multiple of 256
     int units;             // of `packed` in a tile (a dense layer is one tile): its rows in eights; 0: no packed form
+    int s_blocks;          // of `sparse`: ceil(k / 256) blocks; 0: a pattern that keeps more than two of four aligned columns
     float* scales;         // [c_out]
     uint16_t* indices;     // [n_tiles][kk_ld]
     int8_t* packed;        // [tile][unit][kk_ld / 64][8 rows x 4 quarters][16]: retained weights, zeros behind the last column and row; the 512
                            // bytes of a unit and 64 columns are one warp's load, row and quarter by lane.  NULL for tiles of less than 8 rows
     int8_t* expanded;      // [k_blocks][rows][128]: pruned columns are zeros; a row's eight 16-byte pieces stand in the order of the
                            // tensor core's 128-byte swizzle (piece i of row r at i ^ (r & 7))
+    int8_t* sparse;        // [s_blocks][rows][128]: two of every four columns, the others are zeros; pieces as in `expanded`
+    uint8_t* places;       // [s_blocks][rows / 128][4096]: which two, four bits for four columns, 32 bytes a row, as the image that
+                           // tmem_cp_128x256b reads: 8-row groups of two 128-byte halves, 16 bytes of each row in a half
     int* status;           // device int[4], as in nm_weights
 };
 

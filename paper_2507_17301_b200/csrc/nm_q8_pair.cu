@@ -28,23 +28,31 @@ namespace {
 
 using namespace nmk;
 
-constexpr int BN = 256;
-constexpr int A_BYTES = 128 * 128, B_BYTES = BN / 2 * 128, STAGE_BYTES = A_BYTES + B_BYTES;
-constexpr int STAGES = 6;
 constexpr int THREADS = 384;             // 4 service warps + 8 epilogue warps
 constexpr int EPI_TOKENS = 16;           // of an epilogue step
 constexpr int STAGING = EPI_TOKENS * 32 * 4;   // bytes of a warp's box
-constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + 8 * STAGING;
+
+// Tokens of a tile; columns and bytes of a stage.
+template <bool SPARSE>
+struct Shape {
+    static constexpr int BN = SPARSE ? 224 : 256, COLUMNS = SPARSE ? 256 : 128, STAGES = SPARSE ? 4 : 6;
+    static constexpr int A_BYTES = 128 * 128, PLACES = SPARSE ? 4096 : 0, B_BLOCK = BN / 2 * 128, B_BLOCKS = SPARSE ? 2 : 1;
+    static constexpr int B_AT = A_BYTES + PLACES, STAGE_BYTES = B_AT + B_BLOCKS * B_BLOCK;
+    static constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + 8 * STAGING;
+    static constexpr uint32_t PLACES_COLUMN = BN;   // of tensor memory, eight of each stage, behind the first accumulator (the second begins at 256)
+};
+static_assert(Shape<true>::PLACES_COLUMN + 8 * Shape<true>::STAGES <= 256, "");
 
 struct PairArgs {
-    const int8_t* expanded;
+    const int8_t* weights;     // expanded or sparse
+    const uint8_t* places;
     const float* w_scale;
     const float* x_scale;
     const float* bias;
     void* y;
     long long y_ld;
     int* status;
-    int tokens, c_out, rows, k_blocks;
+    int tokens, c_out, rows, blocks;   // blocks: stages of a work item
     uint32_t c_tiles, n_work;
 };
 
@@ -58,9 +66,11 @@ __device__ __forceinline__ uint32_t bits_of(float v)
     else return __bfloat16_as_ushort(__float2bfloat16_rn(v));
 }
 
-template <typename T>
+template <typename T, bool SPARSE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pair(const PairArgs g, const __grid_constant__ CUtensorMap tm_x)
 {
+    using S = Shape<SPARSE>;
+    constexpr int BN = S::BN, STAGES = S::STAGES, STAGE_BYTES = S::STAGE_BYTES, A_BYTES = S::A_BYTES;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t s_full[STAGES], s_free[STAGES], s_accfull[2], s_accfree[2];
     __shared__ uint32_t s_tmem;
@@ -100,15 +110,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pai
             RingPos rp;
             for (uint32_t work = pair; work < g.n_work && !aborted(abort_flag); work += n_pairs) {
                 const uint32_t c_tile = work % g.c_tiles, t_tile = work / g.c_tiles;
-                const int8_t* src = g.expanded + (static_cast<size_t>(c_tile) * 256 + rank * 128) * 128;
+                const int8_t* src = g.weights + (static_cast<size_t>(c_tile) * 256 + rank * 128) * 128;
+                const uint8_t* places = SPARSE ? g.places + static_cast<size_t>(c_tile * 2 + rank) * 4096 : nullptr;
                 const int t0 = static_cast<int>(t_tile * BN + rank * (BN / 2));
-                for (int kb = 0; kb < g.k_blocks; ++kb) {
+                for (int kb = 0; kb < g.blocks; ++kb) {
                     if (rp.wrapped && !mbar_wait_lone(smem_u32(&s_free[rp.s]), rp.parity ^ 1u)) *abort_flag = 2;
                     if (aborted(abort_flag)) break;
                     const uint32_t at = ring + rp.s * STAGE_BYTES, bar = smem_u32(&s_full[rp.s]);
                     mbar_arrive_expect_tx(bar, STAGE_BYTES);
                     bulk_load_1d(at, src, A_BYTES, bar);
-                    tma_load_2d(at + A_BYTES, &tm_x, bar, kb * 128, t0);
+                    if constexpr (SPARSE) {
+                        bulk_load_1d(at + A_BYTES, places, S::PLACES, bar);
+                        places += static_cast<size_t>(g.rows) * 32;
+                    }
+#pragma unroll
+                    for (int b = 0; b < S::B_BLOCKS; ++b)   // (past the last column: zeros)
+                        tma_load_2d(at + S::B_AT + b * S::B_BLOCK, &tm_x, bar, kb * S::COLUMNS + b * 128, t0);
                     src += static_cast<size_t>(g.rows) * 128;
                     rp.advance(STAGES);
                     ++issued;
@@ -129,7 +146,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pai
         if (elect_one()) {
             RingPos rp;
             for (uint32_t work = pair; work < g.n_work && !aborted(abort_flag); work += n_pairs) {
-                for (int kb = 0; kb < g.k_blocks; ++kb) {
+                for (int kb = 0; kb < g.blocks; ++kb) {
                     if (!mbar_wait_lone(smem_u32(&s_full[rp.s]), rp.parity)) { *abort_flag = 4; break; }
                     mbar_arrive_cluster_relaxed(mapa_shared(smem_u32(&s_full[rp.s]), 0));
                     rp.advance(STAGES);
@@ -139,7 +156,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pai
     } else if (warp == 1) {
         // =========================== MMA issuer (first CTA) ===========================
         if (elect_one()) {
-            constexpr uint32_t idesc = umma_idesc_s8(256, BN);
+            constexpr uint32_t idesc = umma_idesc_s8(256, BN) | (SPARSE ? kSparseA : 0u);
             RingPos rp;
             uint32_t ab = 0, acc_par = 0;
             bool acc_wrapped = false;
@@ -149,14 +166,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pai
                     break;
                 }
                 tc_fence_after();
-                const uint32_t acc = tmem + ab * BN;
-                for (int kb = 0; kb < g.k_blocks; ++kb) {
+                const uint32_t acc = tmem + ab * 256;
+                for (int kb = 0; kb < g.blocks; ++kb) {
                     if (!mbar_wait_lone(smem_u32(&s_full[rp.s]), rp.parity)) { *abort_flag = 6; break; }
                     tc_fence_after();
                     const uint32_t at = ring + rp.s * STAGE_BYTES;
-                    const uint64_t adesc = umma_desc_k_sw128(at, 1024), bdesc = umma_desc_k_sw128(at + A_BYTES, 1024);
+                    const uint64_t adesc = umma_desc_k_sw128(at, 1024);
+                    if constexpr (SPARSE) {
+                        // (in order with the MMAs behind it; a stage's columns are free again when its shared memory is)
+                        const uint32_t places = tmem + S::PLACES_COLUMN + 8 * rp.s;
+                        tmem_cp_128x256b_pair(places, umma_desc_k_plain(at + A_BYTES, 128, 256));
 #pragma unroll
-                    for (int kq = 0; kq < 4; ++kq) umma_s8_ss_pair(acc, adesc + 2 * kq, bdesc + 2 * kq, idesc, (kb > 0 || kq > 0) ? 1u : 0u);
+                        for (int kq = 0; kq < 4; ++kq)
+                            umma_s8_sparse_pair(acc, adesc + 2 * kq, umma_desc_k_sw128(at + S::B_AT + kq / 2 * S::B_BLOCK, 1024) + 4 * (kq % 2), places + 2 * kq, idesc,
+                                                (kb > 0 || kq > 0) ? 1u : 0u);
+                    } else {
+                        const uint64_t bdesc = umma_desc_k_sw128(at + S::B_AT, 1024);
+#pragma unroll
+                        for (int kq = 0; kq < 4; ++kq) umma_s8_ss_pair(acc, adesc + 2 * kq, bdesc + 2 * kq, idesc, (kb > 0 || kq > 0) ? 1u : 0u);
+                    }
                     umma_commit_pair(smem_u32(&s_free[rp.s]));
                     rp.advance(STAGES);
                 }
@@ -191,7 +219,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pai
             tc_fence_after();
             for (int blk = half; blk < BN / EPI_TOKENS; blk += 2) {
                 uint32_t v[16];
-                tmem_ld16(mine + ab * BN + blk * EPI_TOKENS, v);
+                tmem_ld16(mine + ab * 256 + blk * EPI_TOKENS, v);
                 const float xs = xs_next;
                 if (blk + 2 < BN / EPI_TOKENS) xs_next = scale_of(blk + 2);
                 tmem_ld_wait();
@@ -259,7 +287,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pai
 }
 
 using Kernel = void (*)(PairArgs, CUtensorMap);
-Kernel kernel_of(nm_dtype_t t) { return t == NM_F32 ? k_q8_pair<float> : t == NM_BF16 ? k_q8_pair<__nv_bfloat16> : k_q8_pair<__half>; }
+template <bool SPARSE>
+Kernel kernel_of(nm_dtype_t t)
+{
+    return t == NM_F32 ? k_q8_pair<float, SPARSE> : t == NM_BF16 ? k_q8_pair<__nv_bfloat16, SPARSE> : k_q8_pair<__half, SPARSE>;
+}
 
 // Pairs of SMs that can hold one cluster each at the same time (0 = clusters unavailable).
 int max_pairs()
@@ -269,7 +301,8 @@ int max_pairs()
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     int n = known[dev].load();
     if (n == 0) {
-        const Kernel kernel = kernel_of(NM_BF16);
+        const Kernel kernel = kernel_of<false>(NM_BF16);
+        constexpr size_t SMEM = Shape<false>::SMEM;   // (either takes a whole SM)
         cudaLaunchConfig_t lc = {};
         lc.gridDim = dim3(2);
         lc.blockDim = dim3(THREADS);
@@ -300,27 +333,31 @@ bool q8_pair_takes(const Q8Linear& p)
     // tokens 17.0 / 19.8; 2048 -> 2048, 1024 tokens 11.7 / 9.1, 2048 tokens 12.8 / 15.0; 4096 -> 12288, 128 tokens 15.3 / 14.1, 200 tokens
     // 16.6 / 19.9.
     const long long small = static_cast<long long>((p.w->c_out + 127) / 128) * ((static_cast<long long>(p.tokens) + 127) / 128);
-    const long long work = static_cast<long long>(p.w->rows / 256) * ((static_cast<long long>(p.tokens) + BN - 1) / BN);
+    const long long work = static_cast<long long>(p.w->rows / 256) * ((static_cast<long long>(p.tokens) + 223) / 224);
     return p.tokens > 128 && small > sm_count() && work < (1ll << 30) && max_pairs() > 0;
 }
 
 nm_status_t launch_q8_pair(const Q8Linear& p, cudaStream_t st)
 {
     const nm_q8_weights* w = p.w;
+    const bool sparse = w->sparse != nullptr;
+    const int bn = sparse ? Shape<true>::BN : Shape<false>::BN;
+    const size_t smem = sparse ? Shape<true>::SMEM : Shape<false>::SMEM;
     PairArgs g = {};
-    g.expanded = w->expanded; g.w_scale = w->scales; g.x_scale = p.x_scale; g.bias = p.bias; g.y = p.y; g.y_ld = p.y_ld; g.status = w->status;
-    g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows; g.k_blocks = w->k_blocks;
+    g.weights = sparse ? w->sparse : w->expanded; g.places = w->places; g.w_scale = w->scales; g.x_scale = p.x_scale; g.bias = p.bias; g.y = p.y;
+    g.y_ld = p.y_ld; g.status = w->status; g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows;
+    g.blocks = sparse ? w->s_blocks : w->k_blocks;
     g.c_tiles = static_cast<uint32_t>(w->rows / 256);
-    g.n_work = g.c_tiles * static_cast<uint32_t>((static_cast<long long>(p.tokens) + BN - 1) / BN);
+    g.n_work = g.c_tiles * static_cast<uint32_t>((static_cast<long long>(p.tokens) + bn - 1) / bn);
     alignas(64) CUtensorMap tm;
-    if (!q8_encode_x(p, BN / 2, &tm)) return fail(NM_ERR_CUDA, "nm_q8_linear: tensor-map encoding failed (pairs)");
-    const Kernel kernel = kernel_of(p.y_type);
-    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), SMEM);
+    if (!q8_encode_x(p, bn / 2, &tm)) return fail(NM_ERR_CUDA, "nm_q8_linear: tensor-map encoding failed (pairs)");
+    const Kernel kernel = sparse ? kernel_of<true>(p.y_type) : kernel_of<false>(p.y_type);
+    cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear: cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     const unsigned pairs_max = static_cast<unsigned>(max_pairs());
     if (pairs_max < 1) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: this device runs no clusters of two CTAs");
     const unsigned pairs = g.n_work < pairs_max ? g.n_work : pairs_max;
-    e = launch_pdl(kernel, 2 * pairs, THREADS, SMEM, st, g, tm);
+    e = launch_pdl(kernel, 2 * pairs, THREADS, smem, st, g, tm);
     count_launch(1);
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear launch (pairs): %s", cudaGetErrorString(e));

@@ -294,3 +294,34 @@ def test_a_gated_block(nm, tokens):
         graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a.cpu(), b.cpu()) for a, b in zip(again, got))
+
+
+@pytest.mark.parametrize("c_out,k,n,m,tile,tokens", [
+    (1001, 300, 2, 4, 64, 2431), (300, 129, 1, 8, 16, 6500), (1500, 513, 3, 4, 32, 1700), (130, 77, 1, 2, 8, 9601), (2304, 1024, 2, 8, 100, 1111),
+    (640, 640, 1, 1, 64, 3900), (4864, 2050, 1, 3, 64, 449), (257, 1, 1, 1, 64, 8000), (2560, 260, 2, 4, 1, 1025), (1024, 512, 4, 8, 64, 2432)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_many_tokens(nm, c_out, k, n, m, tile, tokens, dtype):
+    """More tiles than SMs: pairs of CTAs, with and without sparse operands (two of four columns at most), aligned and unaligned
+    outputs, against sums of integers in 64-bit floating point."""
+    v, s, i = layer(c_out, k, n, m, tile, seed=k)
+    v[1::3, ::2] = 0                                   # retained weights that are zero
+    h = import_layer(nm, v, s, i, k, n, m, tile)
+    x, xs = activations(tokens, k)
+    s = (s / 20).astype(np.float32)                    # (fp16's range)
+    h = import_layer(nm, v, s, i, k, n, m, tile)
+    bias = np.random.default_rng(2).normal(size=c_out).astype(np.float32)
+    dense = torch.from_numpy(ref.dense_of(v, i, k, tile)).cuda()
+    prod = (torch.from_numpy(x).cuda().double() @ dense.T) * torch.from_numpy(xs).cuda().double()[:, None] * torch.from_numpy(s).cuda().double()
+    want = prod + torch.from_numpy(bias).cuda().double()
+    u = 2.0 ** -24
+    limit = prod.abs() * 2 * u * (1 + 4 * u) + want.abs() * u
+    half = ref.STEP[dtype] if dtype != torch.float32 else 0.0
+    limit = limit + (want.abs() + limit) * half + (2.0 ** -25 if dtype == torch.float16 else 2.0 ** -126)
+    assert want.abs().max() < 65000
+    wide = torch.full((tokens + 1, c_out + 3), 7.0, dtype=dtype, device="cuda")
+    for out in (None, wide[:tokens, 1:c_out + 1]):
+        y = nm.nm_q8_linear(h, on_gpu(x), torch.from_numpy(xs).cuda(), bias=torch.from_numpy(bias).cuda(), out_dtype=dtype, y=out)
+        nm.nm_q8_weights_check(h)
+        assert torch.all((y.double() - want).abs() <= limit), ((y.double() - want).abs() / limit).max()
+    wide[:tokens, 1:c_out + 1] = 7.0
+    assert torch.all(wide == 7.0)
