@@ -365,7 +365,7 @@ typedef enum { NM_F32 = 0, NM_BF16 = 1, NM_F16 = 2 } nm_dtype_t;
  *                   Columns h to q_ld are left as they were
  *   scale           device fp32 [tokens]
  * h <= 65535.  Asynchronous on `cuda_stream`, which belongs to the current device like the tensors; allocates nothing.
- * Errors: INVALID_ARG, UNSUPPORTED (h), CUDA.
+ * Errors: INVALID_ARG, UNSUPPORTED (h, more than 2^30 tokens), CUDA.
  */
 nm_status_t nm_q8_rows(const void* x, long long x_ld, nm_dtype_t dtype, int tokens, int h, int8_t* q, long long q_ld,
                        float* scale, void* cuda_stream);
@@ -415,7 +415,7 @@ nm_status_t nm_q8_weights_free(nm_q8_weights_t* w);
  *   y        device [tokens][y_ld] of `y_dtype`, aligned to its elements; overlaps no input
  * A token's output does not depend on the other tokens of the call or on their number.
  * Asynchronous on `cuda_stream` (of the handle's device, which is the current one); allocates nothing.  Calls with one handle may overlap.
- * Errors: INVALID_ARG, CUDA.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^30 tokens, 2^27 tiles), CUDA.
  */
 nm_status_t nm_q8_linear(const nm_q8_weights_t* w, const int8_t* x, long long x_ld, const float* x_scale, int tokens,
                          const float* bias, void* y, long long y_ld, nm_dtype_t y_dtype, void* cuda_stream);

@@ -588,6 +588,17 @@ __device__ __forceinline__ void umma_s8_sparse_pair(uint32_t d_tmem, uint64_t ad
         "l"(adesc), "l"(bdesc), "r"(meta), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+__device__ __forceinline__ void umma_s8_sparse(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t meta, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.sp.cta_group::1.kind::i8 [%0], %1, %2, [%3], %4, p;\n\t"
+        "}\n" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(meta), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 // tmem_cp_128x256b from each CTA's shared memory to its own tensor memory, issued by the first CTA.
 __device__ __forceinline__ void tmem_cp_128x256b_pair(uint32_t taddr, uint64_t sdesc)
 {

@@ -10,6 +10,8 @@ namespace {
 
 using nmhost::fail;
 
+constexpr int kMostTokens = 1 << 30;
+
 size_t size_of(nm_dtype_t t) { return t == NM_F32 ? 4 : 2; }
 bool known(nm_dtype_t t) { return t == NM_F32 || t == NM_BF16 || t == NM_F16; }
 uintptr_t at(const void* p) { return reinterpret_cast<uintptr_t>(p); }
@@ -41,6 +43,7 @@ nm_status_t run_rows(const char* who, Q8RowOp op, Q8Rows a, nm_dtype_t type, nm_
     if (!known(type) || !known(weight_type)) return fail(NM_ERR_INVALID_ARG, "%s: unknown type", who);
     if (a.tokens < 0 || a.h < 1) return fail(NM_ERR_INVALID_ARG, "%s: need tokens >= 0 and h >= 1", who);
     if (a.h > 65535) return fail(NM_ERR_UNSUPPORTED, "%s: h = %d exceeds 65535", who, a.h);
+    if (a.tokens > kMostTokens) return fail(NM_ERR_UNSUPPORTED, "%s: more than 2^30 tokens", who);
     if (a.tokens == 0) return NM_OK;
     if (!a.x || !a.q || !a.scale) return fail(NM_ERR_INVALID_ARG, "%s: a tensor is NULL", who);
     const size_t size = size_of(type);
@@ -495,6 +498,7 @@ nm_status_t nm_q8_linear(const nm_q8_weights_t* w, const int8_t* x, long long x_
     if (!valid(w)) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: bad weights handle");
     if (!known(y_dtype)) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: unknown type");
     if (tokens < 0) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: tokens must be >= 0");
+    if (tokens > kMostTokens) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: more than 2^30 tokens");
     if (tokens == 0) return NM_OK;
     if (!x || !x_scale || !y) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: x, x_scale or y is NULL");
     if (tokens == 1) {

@@ -290,14 +290,16 @@ struct FewPlan {
 };
 
 // Which calls the kernel takes, and its rows a block.  Every block gathers all columns for its rows, so that the tokens it pays for go by
-// its rows; against the tensor-memory kernel, us: 4096 -> 4096 at 2:4 in tiles of 64, eight tokens 4.2 / 6.7; in tiles of 8, four tokens
-// 6.4 / 6.7, eight 7.8 / 6.7; dense, four tokens 5.5 / 6.8, eight 7.9 / 6.9; 8192 -> 2048 at 1:4, eight tokens 4.3 / 10.5.
-// Blocks of 32 rows where 16 would be more than two an SM (4096 -> 12288 at 2:4: one token 5.3 us against 7.1, eight 7.5 against 12).
+// its rows; against the tensor-memory kernel, us: 4096 -> 4096 at 2:4 in tiles of 64, one token 3.2 / 5.2, eight 4.4 / 5.2; in tiles of 8
+// one token 5.9 / 5.1, but 1000 -> 1001 at 2:8 in tiles of 8 1.8 / 2.8; dense 4096 -> 4096, four tokens 5.5 / 6.8, eight 7.9 / 6.9;
+// 8192 -> 2048 at 1:4, eight tokens 4.7 / 4.6.
+// Blocks of 32 rows where 16 would be more than two an SM (4096 -> 12288 at 2:4: one token 5.5 us against 7.1, eight 7.5 against 12).
 bool plan(const Q8Linear& p, FewPlan* f)
 {
     const nm_q8_weights* w = p.w;
     const bool dense = w->n_keep == w->m_group;
     if (!w->packed || p.tokens > (dense || w->units < 2 ? 4 : 8)) return false;
+    if (w->units < 2 && w->sparse && w->n_tiles > 2 * nmhost::sm_count()) return false;
     f->tokens = p.tokens <= 2 ? p.tokens : p.tokens <= 4 ? 4 : 8;
     const int tiles = dense ? 1 : w->n_tiles;
     f->units = w->units >= 4 && static_cast<long long>(tiles) * ((w->units + 1) / 2) > 2 * nmhost::sm_count() ? 4 : 2;

@@ -25,20 +25,24 @@ using namespace nmk;
 constexpr int THREADS = 192;   // warps: 0 producer, 1 MMA issuer and tensor memory, 2-5 epilogue
 constexpr int NSTAGE_MAX = 8;
 constexpr int A_BYTES = 128 * 128;
+constexpr int PLACES = 4096;   // bytes of a sparse stage's places
 
 struct GemmArgs {
-    const int8_t* expanded;
+    const int8_t* weights;     // expanded or sparse
+    const uint8_t* places;
     const float* w_scale;
     const float* x_scale;
     const float* bias;
     void* y;
     long long y_ld;
     int* status;
-    int tokens, c_out, rows, k_blocks;
+    int tokens, c_out, rows;
+    int blocks;   // of the reduction axis: 128 columns, 256 of sparse weights
     int c_tiles;
     int bn;
     int ks;       // CTAs of a cluster = ranges of the reduction axis
     int stages, stage_bytes;
+    int tmem;     // columns of tensor memory
 };
 
 template <typename T>
@@ -76,7 +80,7 @@ __device__ __forceinline__ int4 load_int4(uint32_t at)
     return v;
 }
 
-template <typename T>
+template <typename T, bool SPARSE>
 __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const __grid_constant__ CUtensorMap tm_x)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -90,12 +94,12 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
     const int item = static_cast<int>(blockIdx.x) / g.ks;
     const int c0 = item % g.c_tiles * 128;                 // consecutive items share their tokens
     const int t0 = item / g.c_tiles * g.bn;
-    const int kb0 = static_cast<int>(static_cast<long long>(g.k_blocks) * rank / g.ks), kb1 = static_cast<int>(static_cast<long long>(g.k_blocks) * (rank + 1) / g.ks);
+    const int kb0 = static_cast<int>(static_cast<long long>(g.blocks) * rank / g.ks), kb1 = static_cast<int>(static_cast<long long>(g.blocks) * (rank + 1) / g.ks);
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t recv = ring + g.stages * g.stage_bytes;   // [ks][bn / ks tokens][128 channels] (ks > 1)
     volatile int* abort_flag = &s_abort;
 
-    if (warp == 1) tmem_alloc(smem_u32(&s_tmem), g.bn < 32 ? 32 : g.bn);
+    if (warp == 1) tmem_alloc(smem_u32(&s_tmem), g.tmem);
     if (tid == 0) {
         for (int i = 0; i < NSTAGE_MAX; ++i) {
             mbar_init(smem_u32(&s_full[i]), 1);
@@ -117,19 +121,28 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
 
     if (warp == 0) {
         if (elect_one()) {
-            const int8_t* src = g.expanded + (static_cast<size_t>(kb0) * g.rows + c0) * 128;
-            const uint32_t tx = static_cast<uint32_t>(A_BYTES + g.bn * 128);
+            const int8_t* src = g.weights + (static_cast<size_t>(kb0) * g.rows + c0) * 128;
+            const uint8_t* places = SPARSE ? g.places + (static_cast<size_t>(kb0) * g.rows + c0) * 32 : nullptr;
             RingPos rp;
             int issued = 0;
             bool after = false;   // the kernel before has ended
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (rp.wrapped && !mbar_wait_lone(smem_u32(&s_free[rp.s]), rp.parity ^ 1u)) { *abort_flag = 1; break; }
                 const uint32_t at = ring + rp.s * g.stage_bytes, bar = smem_u32(&s_full[rp.s]);
-                mbar_arrive_expect_tx(bar, tx);
+                mbar_arrive_expect_tx(bar, static_cast<uint32_t>(g.stage_bytes));
                 bulk_load_1d(at, src, A_BYTES, bar);   // weights: no kernel of the stream writes them
+                if constexpr (SPARSE) {
+                    bulk_load_1d(at + A_BYTES, places, PLACES, bar);
+                    places += static_cast<size_t>(g.rows) * 32;
+                }
                 if (!after) pdl_wait();
                 after = true;
-                tma_load_2d(at + A_BYTES, &tm_x, bar, kb * 128, t0);
+                if constexpr (SPARSE) {   // (past the last column: zeros)
+                    tma_load_2d(at + A_BYTES + PLACES, &tm_x, bar, kb * 256, t0);
+                    tma_load_2d(at + A_BYTES + PLACES + g.bn * 128, &tm_x, bar, kb * 256 + 128, t0);
+                } else {
+                    tma_load_2d(at + A_BYTES, &tm_x, bar, kb * 128, t0);
+                }
                 src += static_cast<size_t>(g.rows) * 128;
                 rp.advance(g.stages);
                 ++issued;
@@ -146,15 +159,26 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
         }
     } else if (warp == 1) {
         if (elect_one()) {
-            const uint32_t idesc = umma_idesc_s8(128, g.bn);
+            const uint32_t idesc = umma_idesc_s8(128, g.bn) | (SPARSE ? kSparseA : 0u);
             RingPos rp;
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait_lone(smem_u32(&s_full[rp.s]), rp.parity)) { *abort_flag = 2; break; }
                 tc_fence_after();
                 const uint32_t at = ring + rp.s * g.stage_bytes;
-                const uint64_t adesc = umma_desc_k_sw128(at, 1024), bdesc = umma_desc_k_sw128(at + A_BYTES, 1024);
+                const uint64_t adesc = umma_desc_k_sw128(at, 1024);
+                if constexpr (SPARSE) {
+                    // (in order with the MMAs behind it; a stage's columns are free again when its shared memory is)
+                    const uint32_t places = tmem + g.bn + 8 * rp.s;
+                    tmem_cp_128x256b(places, umma_desc_k_plain(at + A_BYTES, 128, 256));
 #pragma unroll
-                for (int kq = 0; kq < 4; ++kq) umma_s8_ss(tmem, adesc + 2 * kq, bdesc + 2 * kq, idesc, (kb > kb0 || kq > 0) ? 1u : 0u);
+                    for (int kq = 0; kq < 4; ++kq)
+                        umma_s8_sparse(tmem, adesc + 2 * kq, umma_desc_k_sw128(at + A_BYTES + PLACES + kq / 2 * g.bn * 128, 1024) + 4 * (kq % 2), places + 2 * kq, idesc,
+                                       (kb > kb0 || kq > 0) ? 1u : 0u);
+                } else {
+                    const uint64_t bdesc = umma_desc_k_sw128(at + A_BYTES, 1024);
+#pragma unroll
+                    for (int kq = 0; kq < 4; ++kq) umma_s8_ss(tmem, adesc + 2 * kq, bdesc + 2 * kq, idesc, (kb > kb0 || kq > 0) ? 1u : 0u);
+                }
                 umma_commit(smem_u32(&s_free[rp.s]));
                 rp.advance(g.stages);
             }
@@ -233,7 +257,14 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
         atomicExch(g.status + 1, 200 + s_abort);
         atomicExch(g.status + 2, static_cast<int>(blockIdx.x));
     }
-    if (warp == 1) tmem_dealloc(tmem, g.bn < 32 ? 32 : g.bn);
+    if (warp == 1) tmem_dealloc(tmem, g.tmem);
+}
+
+using Kernel = void (*)(GemmArgs, CUtensorMap);
+template <bool SPARSE>
+Kernel kernel_of(nm_dtype_t t)
+{
+    return t == NM_F32 ? k_q8_gemm<float, SPARSE> : t == NM_BF16 ? k_q8_gemm<__nv_bfloat16, SPARSE> : k_q8_gemm<__half, SPARSE>;
 }
 
 }  // namespace
@@ -255,25 +286,30 @@ nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
 {
     const nm_q8_weights* w = p.w;
     GemmArgs g = {};
-    g.expanded = w->expanded; g.w_scale = w->scales; g.x_scale = p.x_scale; g.bias = p.bias; g.y = p.y; g.y_ld = p.y_ld; g.status = w->status;
-    g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows; g.k_blocks = w->k_blocks;
+    const bool sparse = w->sparse != nullptr;
+    g.weights = sparse ? w->sparse : w->expanded; g.places = w->places; g.w_scale = w->scales; g.x_scale = p.x_scale; g.bias = p.bias; g.y = p.y; g.y_ld = p.y_ld; g.status = w->status;
+    g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows;
+    g.blocks = sparse ? w->s_blocks : w->k_blocks;
     g.c_tiles = (w->c_out + 127) / 128;
     // The narrowest tiles that still are one round, us: 4096 -> 4096, 128 tokens in tiles of 16 / 32 / 64 / 128: 16.0 / 8.7 / 9.2 / 11.1; 512 tokens:
     // 56 / 34 / 19 / 12.2.  A split of the reduction axis pays where half the SMs would idle (16 tokens, 2048 -> 2048: 5.0 whole, 3.8 in
     // four), not in eight (7.9).
     g.bn = 16;
-    while (g.bn < 256 && g.bn < p.tokens && static_cast<long long>(g.c_tiles) * ((p.tokens + g.bn - 1) / g.bn) > sm_count()) g.bn *= 2;
-    const long long items = static_cast<long long>(g.c_tiles) * ((p.tokens + g.bn - 1) / g.bn);
+    auto items_of = [&](int bn) { return static_cast<long long>(g.c_tiles) * ((p.tokens + bn - 1) / bn); };
+    while (g.bn < 256 && g.bn < p.tokens && items_of(g.bn) > sm_count()) g.bn *= 2;
+    const long long items = items_of(g.bn);
     if (items > (1ll << 27)) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: too many tiles");
     g.ks = 1;
-    while (g.bn <= 128 && g.ks < 4 && items * g.ks * 2 <= sm_count() && g.k_blocks >= g.ks * 4) g.ks *= 2;
+    while (g.bn <= 128 && g.ks < 4 && items * g.ks * 2 <= sm_count() && g.blocks * (sparse ? 2 : 1) >= g.ks * 4) g.ks *= 2;
     // More than a round of CTAs: two on an SM, one sets up and loads while the other finishes (in one round the deeper ring is faster:
     // 4096 -> 4096, 512 tokens 12.2 us against 16.9)
     const bool half = g.bn <= 128 && items > sm_count();
-    g.stage_bytes = A_BYTES + g.bn * 128;
+    g.stage_bytes = sparse ? A_BYTES + PLACES + 2 * g.bn * 128 : A_BYTES + g.bn * 128;
     const int budget = (half ? 112 : 224) * 1024 - 1024 - 2048 - (g.ks > 1 ? g.bn * 512 : 0);
     g.stages = std::min(NSTAGE_MAX, budget / g.stage_bytes);
-    // (the sums of a tile, bn * 512 bytes, go through the ring, which has at least 96 KB, 192 KB with bn = 256)
+    // (the sums of a tile, bn * 512 bytes, go through the ring, which has at least 96 KB, 168 KB with bn = 256)
+    g.tmem = 32;
+    while (g.tmem < g.bn + (sparse ? 8 * g.stages : 0)) g.tmem *= 2;
     alignas(64) CUtensorMap tm;
     if (!q8_encode_x(p, g.bn, &tm)) return fail(NM_ERR_CUDA, "nm_q8_linear: tensor-map encoding failed");
     size_t smem = 1024 + static_cast<size_t>(g.stages) * g.stage_bytes + (g.ks > 1 ? g.bn * 512 : 0);
@@ -281,7 +317,7 @@ nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
     // that take all of it leave free.
     if (!half && smem < NM_EXCLUSIVE_SMEM) smem = NM_EXCLUSIVE_SMEM;
     if (half && smem < 76 * 1024) smem = 76 * 1024;   // (at most two on an SM, of 256 columns of tensor memory at most)
-    void (*kernel)(GemmArgs, CUtensorMap) = p.y_type == NM_F32 ? k_q8_gemm<float> : p.y_type == NM_BF16 ? k_q8_gemm<__nv_bfloat16> : k_q8_gemm<__half>;
+    const Kernel kernel = sparse ? kernel_of<true>(p.y_type) : kernel_of<false>(p.y_type);
     cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear: cudaFuncSetAttribute: %s", cudaGetErrorString(e));
     cudaLaunchConfig_t cfg = {};

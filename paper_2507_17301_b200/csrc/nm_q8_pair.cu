@@ -39,9 +39,9 @@ struct Shape {
     static constexpr int A_BYTES = 128 * 128, PLACES = SPARSE ? 4096 : 0, B_BLOCK = BN / 2 * 128, B_BLOCKS = SPARSE ? 2 : 1;
     static constexpr int B_AT = A_BYTES + PLACES, STAGE_BYTES = B_AT + B_BLOCKS * B_BLOCK;
     static constexpr size_t SMEM = 1024 + STAGES * STAGE_BYTES + 8 * STAGING;
-    static constexpr uint32_t PLACES_COLUMN = BN;   // of tensor memory, eight of each stage, behind the first accumulator (the second begins at 256)
 };
-static_assert(Shape<true>::PLACES_COLUMN + 8 * Shape<true>::STAGES <= 256, "");
+// places in tensor memory: eight columns of each stage behind the first accumulator (the second begins at 256)
+static_assert(Shape<true>::BN + 8 * Shape<true>::STAGES <= 256, "");
 
 struct PairArgs {
     const int8_t* weights;     // expanded or sparse
@@ -174,7 +174,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_q8_pai
                     const uint64_t adesc = umma_desc_k_sw128(at, 1024);
                     if constexpr (SPARSE) {
                         // (in order with the MMAs behind it; a stage's columns are free again when its shared memory is)
-                        const uint32_t places = tmem + S::PLACES_COLUMN + 8 * rp.s;
+                        const uint32_t places = tmem + BN + 8 * rp.s;
                         tmem_cp_128x256b_pair(places, umma_desc_k_plain(at + A_BYTES, 128, 256));
 #pragma unroll
                         for (int kq = 0; kq < 4; ++kq)
