@@ -383,7 +383,7 @@ typedef struct nm_q8_weights nm_q8_weights_t;
  * w_dense[c_out][k], and the retained weights of every row (output channel) as 8-bit integers:
  *   scale[o] = max_j |w[o][idx_j]| / 127,   values[o][j] = the integer nearest to w[o][idx_j] / scale[o] (ties to even, from
  *   the exact quotient).  A channel of zeros has scale 0, one with a NaN or an infinity scale NaN (its outputs are NaN).
- * n_keep = m_group leaves the layer dense.  Allocates device memory and synchronises `cuda_stream`.
+ * n_keep = m_group leaves the layer dense.  w_dense lies on the current device.  Allocates device memory and synchronises `cuda_stream`.
  * Errors: as nm_prune; k, tile_t limits alike (k <= 65535, tile_t <= 256), c_out / tile_t at most 65535 tiles.
  */
 nm_status_t nm_q8_prune(const float* w_dense, int c_out, int k, int n_keep, int m_group, int tile_t, void* cuda_stream,

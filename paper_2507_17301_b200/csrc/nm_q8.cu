@@ -387,6 +387,10 @@ nm_status_t nm_q8_prune(const float* w_dense, int c_out, int k, int n_keep, int 
     nm_q8_weights* h = nullptr;
     nm_status_t s = make("nm_q8_prune", c_out, k, n_keep, m_group, tile_t, &h);
     if (s != NM_OK) return s;
+    if (!nmhost::kernel_may_touch(w_dense, w_dense, h->device)) {
+        discard(h, true);
+        return fail(NM_ERR_INVALID_ARG, "nm_q8_prune: w_dense must lie on the current device");
+    }
     // scores (fp64) and keep flags of every (tile, column), values
     const size_t cells = static_cast<size_t>(h->n_tiles) * k, want = cells * 9 + static_cast<size_t>(c_out) * h->kk;
     size_t scratch_bytes = 0;
@@ -422,9 +426,9 @@ nm_status_t nm_q8_weights_import(const int8_t* values, const float* scales, cons
     nm_q8_weights* h = nullptr;
     nm_status_t s = make("nm_q8_weights_import", c_out, k, n_keep, m_group, tile_t, &h);
     if (s != NM_OK) return s;
-    if (!nmhost::kernel_may_touch(values, indices, h->device)) {
+    if (!nmhost::kernel_may_touch(values, indices, h->device) || !nmhost::kernel_may_touch(scales, scales, h->device)) {
         discard(h, true);
-        return fail(NM_ERR_INVALID_ARG, "nm_q8_weights_import: values and indices must lie on the current device");
+        return fail(NM_ERR_INVALID_ARG, "nm_q8_weights_import: values, scales and indices must lie on the current device");
     }
     const cudaError_t e = cudaMemcpyAsync(h->scales, scales, static_cast<size_t>(c_out) * 4, cudaMemcpyDeviceToDevice, st);
     s = e == cudaSuccess ? finish("nm_q8_weights_import", h, values, indices, st) : fail(NM_ERR_CUDA, "nm_q8_weights_import: %s", cudaGetErrorString(e));

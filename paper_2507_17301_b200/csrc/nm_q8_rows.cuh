@@ -151,7 +151,7 @@ __device__ __forceinline__ Pair two_of(const Eight<T>& e, int i)
 template <Q8RowOp OP>
 constexpr float kError = OP == Q8_SILU_MUL ? 1.5e-5f : 4e-7f;
 // silu_mul beyond g = -87: less than kMostProduct * 2^-125 * 88, which is nothing beside kLeastTop
-constexpr float kMostProduct = 0x1p20f, kLeastTop = 0x1p-60f;
+constexpr float kMostProduct = 0x1p40f, kLeastTop = 0x1p-60f;
 constexpr float kMostTop = 0x1p100f;   // (127 p and 1 / a stay normal numbers)
 constexpr float kMostSum = 0x1p120f;
 // How near 127 p / a may come to a border between two integers, beside its own error, before 64 bits decide.

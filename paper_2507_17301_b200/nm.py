@@ -389,9 +389,10 @@ def nm_autotune_tile(w_dense: torch.Tensor, n_keep: int, m_group: int, tile_cand
 class Q8Weights:
     """Owner of one ``nm_q8_weights_t*`` handle (freed with the object)."""
 
-    def __init__(self, handle: int):
+    def __init__(self, handle: int, device: torch.device):
         self._h = ctypes.c_void_p(handle)
         self._addr = handle or 0
+        self.device = device
         out = [ctypes.c_int() for _ in range(5)]
         _check(_lib.nm_q8_weights_dims(self._h, *[ctypes.byref(d) for d in out]))
         self.c_out, self.k, self.kk, self.n_tiles, self.tile_t = (d.value for d in out)
@@ -413,11 +414,6 @@ class Q8Weights:
             pass
 
 
-def _on_device(t: torch.Tensor):
-    """The tensor's device as the current one (handles are made on, and belong to, the current device)."""
-    return torch.cuda.device(t.device)
-
-
 def nm_q8_prune(w_dense: torch.Tensor, n_keep: int, m_group: int, tile_t: int) -> Q8Weights:
     """``w_dense``: CUDA fp32 ``[c_out, k]``.  Column-wise N:M pruning as ``nm_prune`` does it, the retained weights in 8-bit
     integers with a scale for each output channel.  ``n_keep = m_group`` leaves the layer dense."""
@@ -425,9 +421,9 @@ def nm_q8_prune(w_dense: torch.Tensor, n_keep: int, m_group: int, tile_t: int) -
     if w_dense.dim() != 2:
         raise TypeError("w_dense must be [c_out, k]")
     out = ctypes.c_void_p()
-    with _on_device(w_dense):
+    with torch.cuda.device(w_dense.device):   # (a handle belongs to the current device)
         _check(_lib.nm_q8_prune(ptr, *w_dense.shape, n_keep, m_group, tile_t, _stream(), ctypes.byref(out)))
-    return Q8Weights(out.value)
+    return Q8Weights(out.value, w_dense.device)
 
 
 def nm_q8_weights_import(values: torch.Tensor, scales: torch.Tensor, indices: torch.Tensor, k: int, n_keep: int, m_group: int,
@@ -446,23 +442,25 @@ def nm_q8_weights_import(values: torch.Tensor, scales: torch.Tensor, indices: to
             raise TypeError("values, scales and indices must be " + ", ".join(str(list(shape)) for _, shape in want)
                             + f" (got {', '.join(str(list(t.shape)) for t, _ in want)})")
     out = ctypes.c_void_p()
-    with _on_device(values):
+    with torch.cuda.device(values.device):
         _check(_lib.nm_q8_weights_import(values.data_ptr(), scales.data_ptr(), indices.data_ptr(), c_out, k, n_keep, m_group, tile_t,
                                          _stream(), ctypes.byref(out)))
-    return Q8Weights(out.value)
+    return Q8Weights(out.value, values.device)
 
 
 def nm_q8_weights_export(w: Q8Weights):
-    """Returns ``(values [c_out, kk] int8, scales [c_out] fp32, indices [n_tiles, kk] uint16)`` on the current device."""
-    values = torch.empty((w.c_out, w.kk), dtype=torch.int8, device="cuda")
-    scales = torch.empty(w.c_out, dtype=torch.float32, device="cuda")
-    indices = torch.empty((w.n_tiles, w.kk), dtype=torch.uint16, device="cuda")
-    _check(_lib.nm_q8_weights_export(w.handle, values.data_ptr(), scales.data_ptr(), indices.data_ptr(), _stream()))
+    """Returns ``(values [c_out, kk] int8, scales [c_out] fp32, indices [n_tiles, kk] uint16)`` on the handle's device."""
+    with torch.cuda.device(w.device):
+        values = torch.empty((w.c_out, w.kk), dtype=torch.int8, device=w.device)
+        scales = torch.empty(w.c_out, dtype=torch.float32, device=w.device)
+        indices = torch.empty((w.n_tiles, w.kk), dtype=torch.uint16, device=w.device)
+        _check(_lib.nm_q8_weights_export(w.handle, values.data_ptr(), scales.data_ptr(), indices.data_ptr(), _stream()))
     return values, scales, indices
 
 
 def nm_q8_weights_check(w: Q8Weights):
-    _check(_lib.nm_q8_weights_check(w.handle, _stream()))
+    with torch.cuda.device(w.device):
+        _check(_lib.nm_q8_weights_check(w.handle, _stream()))
 
 
 def _q8_out(made):

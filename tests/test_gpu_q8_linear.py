@@ -325,3 +325,47 @@ def test_many_tokens(nm, c_out, k, n, m, tile, tokens, dtype):
         assert torch.all((y.double() - want).abs() <= limit), ((y.double() - want).abs() / limit).max()
     wide[:tokens, 1:c_out + 1] = 7.0
     assert torch.all(wide == 7.0)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 4, 8, 15, 70, 1400])
+@pytest.mark.parametrize("n,m", [(2, 4), (1, 1)])
+def test_the_least_integers(nm, tokens, n, m):
+    """-128 on both sides, which the quantising operators never make but a checkpoint may hold: sums of 2^14 a column."""
+    k, c_out = 2050, 1560
+    _, s, i = layer(c_out, k, n, m, 40)
+    v = np.full((c_out, i.shape[1]), -128, dtype=np.int8)
+    h = import_layer(nm, v, s, i, k, n, m, 40)
+    x = np.full((tokens, k), -128, dtype=np.int8)
+    x[tokens // 2, ::3] = 127
+    xs = np.ones(tokens, dtype=np.float32)
+    y = nm.nm_q8_linear(h, on_gpu(x), torch.from_numpy(xs).cuda(), out_dtype=torch.float32)
+    check(y, x, xs, ref.dense_of(v, i, k, 40), s, None, torch.float32)
+
+
+def test_more_sums_than_32_bit_floats_hold(nm):
+    """Eight tokens of a long layer: a warp's part of the columns is more than fp32 adds up exactly at a time."""
+    k, c_out = 40000, 64
+    v, s, i = layer(c_out, k, 2, 4, 32)
+    v[:] = np.where(np.random.default_rng(5).random(v.shape) < 0.5, 127, 126).astype(np.int8)
+    h = import_layer(nm, v, s, i, k, 2, 4, 32)
+    x = np.full((8, k), 127, dtype=np.int8)
+    x[:, 1::7] = 125
+    xs = np.ones(8, dtype=np.float32)
+    for tokens in (1, 2, 3, 5, 8):
+        y = nm.nm_q8_linear(h, on_gpu(x[:tokens]), torch.from_numpy(xs[:tokens]).cuda(), out_dtype=torch.float32)
+        check(y, x[:tokens], xs[:tokens], ref.dense_of(v, i, k, 32), s, None, torch.float32)
+
+
+def test_pruning_rules_of_four_columns(nm):
+    """Sparse operands need at most two retained columns of four aligned ones, whatever the weights: patterns on either side of
+    that, and wherever the columns lie."""
+    for n, m in ((1, 2), (1, 3), (2, 5), (2, 6), (2, 7), (2, 8), (3, 8), (3, 12), (1, 6), (5, 16)):
+        k, c_out, tokens = 333, 200, 40
+        v, s, i = layer(c_out, k, n, m, 16, seed=n * m)
+        for t in range(i.shape[0]):                                    # columns pushed together at one end of each group
+            if t % 3:
+                i[t] = [g + (c if t % 3 == 1 else min(m, k - g) - min(n, k - g) + c) for g in range(0, k, m) for c in range(min(n, k - g))]
+        h = import_layer(nm, v, s, i, k, n, m, 16)
+        x, xs = activations(tokens, k)
+        y = nm.nm_q8_linear(h, on_gpu(x), torch.from_numpy(xs).cuda(), out_dtype=torch.float32)
+        check(y, x, xs, ref.dense_of(v, i, k, 16), s, None, torch.float32)

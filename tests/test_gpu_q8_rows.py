@@ -244,3 +244,69 @@ def test_another_stream_and_a_captured_call(nm):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(q, want[0]) and torch.equal(s, want[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("h", [1, 5, 13, 100, 511, 1001, 1500, 2047, 3001, 4093, 6001, 8187, 12285, 16379, 16391, 20011, 30001, 40003])
+@pytest.mark.parametrize("tokens", [2, 310])
+def test_ragged_rows_16_bytes_apart(nm, dtype, h, tokens):
+    """Rows that end inside a 16-byte piece but begin on one: all operators, every shape of the kernel."""
+    if tokens > 2 and h > 17000:
+        tokens = 299
+    ld = -(-h // 8) * 8 + 8
+    full = [2 * randn(tokens, ld, seed=20 + i, dtype=dtype) for i in range(2)]
+    x, r = (t.cuda()[:, :h] for t in full)
+    w = randn(h, seed=22, dtype=dtype)
+    q, s, out = nm.nm_q8_rmsnorm(x, w.cuda(), 1e-6, residual=r)
+    want_q, want_s, want_r = ref.rmsnorm(full[0][:, :h], w, 1e-6, full[1][:, :h])
+    assert torch.equal(out.cpu(), want_r) and torch.equal(q.cpu(), want_q)
+    same_scale(s, want_s, norm_limit(h))
+    q, s = nm.nm_q8_rmsnorm(x, w.cuda(), 1e-6)
+    want_q, want_s = ref.rmsnorm(full[0][:, :h], w, 1e-6)
+    assert torch.equal(q.cpu(), want_q)
+    same_scale(s, want_s, norm_limit(h))
+    q, s = nm.nm_q8_silu_mul(x, r)
+    want_q, want_s = ref.silu_mul(full[0][:, :h], full[1][:, :h])
+    assert torch.equal(q.cpu(), want_q)
+    same_scale(s, want_s, 2.0 ** -24)
+    q, s = nm.nm_q8_rows(x)
+    want_q, want_s = ref.rows(full[0][:, :h])
+    assert torch.equal(q.cpu(), want_q)
+    same_scale(s, want_s, 2.0 ** -24)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("h", [40, 600, 4096, 9000])
+def test_long_batches_with_rows_out_of_the_ordinary(nm, dtype, h):
+    """Blocks that take many rows each, among them padding, rows that are not finite, tiny and huge ones."""
+    tokens = 5000 if h < 5000 else 2000
+    x, u = randn(tokens, h, seed=30, dtype=dtype), randn(tokens, h, seed=31, dtype=dtype)
+    kind = torch.randint(0, 12, (tokens,), generator=torch.Generator().manual_seed(32))
+    x[kind == 0] = 0
+    x[kind == 1, h // 3] = float("nan")
+    x[kind == 2, h - 1] = float("inf")
+    x[kind == 3] = torch.finfo(dtype).max
+    x[kind == 4] *= 1e-4
+    x[kind == 5, 0] = -100.0                         # a gate far out
+    u[kind == 6, 1] = 2e4                            # a product that stands out
+    w = randn(h, seed=33, dtype=dtype)
+    want = [ref.rmsnorm(x, w, 1e-6), ref.silu_mul(x, u), ref.rows(x)]
+    got = [nm.nm_q8_rmsnorm(x.cuda(), w.cuda(), 1e-6), nm.nm_q8_silu_mul(x.cuda(), u.cuda()), nm.nm_q8_rows(x.cuda())]
+    for (want_q, want_s), (q, s), limit in zip(want, got, (norm_limit(h), 2.0 ** -24, 2.0 ** -24)):
+        bad = ~(want_s <= 3.4e38)
+        assert torch.equal(torch.isnan(s.cpu()), bad) and not q.cpu()[bad].any()
+        assert torch.equal(q.cpu()[~bad], want_q[~bad])
+        same_scale(s[~bad.cuda()], want_s[~bad], limit)
+
+
+def test_calls_on_two_streams_at_once(nm):
+    x = [randn(3000, 1000, seed=40 + i, dtype=torch.bfloat16).cuda() for i in range(2)]
+    want = [nm.nm_q8_silu_mul(x[i], x[1 - i]) for i in range(2)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(8):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(nm.nm_q8_silu_mul(x[i], x[1 - i]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(q, want[i][0]) and torch.equal(s, want[i][1]) for i in range(2) for q, s in got[i])
