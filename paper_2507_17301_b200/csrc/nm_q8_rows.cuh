@@ -223,7 +223,7 @@ __device__ __forceinline__ float border_of(float p, float inv, uint32_t* k)
 {
     const float n = fmaf(p, inv, kRound), whole = n - kRound;
     *k = __float_as_uint(n);
-    return fmaf(fabsf(whole), kError<OP>, fabsf(fmaf(p, inv, -whole)));
+    return fmaf(fabsf(whole), 2.f * kError<OP>, fabsf(fmaf(p, inv, -whole)));   // (the maximum's error beside p's)
 }
 // One column's integer, which 32 bits left open, in 64 bits; top = 0: |p| itself instead.  x_at, r_at: where the column's inputs
 // lie in shared memory (0: read them from global memory, which takes longer).
@@ -262,7 +262,10 @@ __device__ __forceinline__ uint32_t which(const Pair (&p)[4], F&& f)
     return bits;
 }
 
-struct Scratch {
+// (a multiple of 128 bytes: the copied pieces lie behind it, and off a 128-byte boundary a warp's 512 bytes take a pass more: 8192 x 8192
+// bf16 with residual 104 us instead of 90)
+struct alignas(128) Scratch {
+    unsigned long long top64;   // bits of the maximum in 64 bits
     float sum[32];
     uint32_t top[32];
     double a[32], sum64[32];
@@ -522,6 +525,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             sc->sum[t >> 5] = sum;
             sc->top[t >> 5] = top_bits;
         }
+        if (!EXACT && t == 0) sc->top64 = 0ull;
         __syncthreads();
         const int lane = t & 31;
         top_bits = __reduce_max_sync(0xFFFFFFFFu, lane < TPR / 32 ? sc->top[lane] : 0u);
@@ -566,14 +570,26 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             for (int base = t; base * 8 < a.h; base += NV * TPR)
                 pass(base, false, [&](int, int v, Pair (&f)[4]) { look(which(f, is_near), v); });
         }
-        a64 = row_max<TPR>(mine, sc->a);
+        // The maximum in 64 bits decides only where 32 leave a quotient open: it is collected while all threads go on with the one in 32
+        // (of a row that is read again at once, for the decisions are made on the way)
+        if constexpr (TPR == 32) {
+            a64 = warp_max(mine);
+        } else {
+            if (mine > 0.0) atomicMax(&sc->top64, static_cast<unsigned long long>(__double_as_longlong(mine)));
+            if constexpr (!KEEP) {
+                __syncthreads();
+                a64 = __longlong_as_double(static_cast<long long>(sc->top64));
+            }
+        }
     }
-    if (t == 0) {
-        float scale = static_cast<float>(a64 / 127.0);
+    auto write_scale = [&] {
+        if (t != 0) return;
+        float scale = EXACT ? a32 / 127.f : static_cast<float>(a64 / 127.0);
         if constexpr (OP == Q8_RMSNORM) scale *= 1.f / sqrtf(sum / static_cast<float>(a.h) + a.eps);
         a.scale[row] = scale < INFINITY ? scale : NAN;
-    }
-    const float a32_top = static_cast<float>(a64), rcp = __frcp_rn(a32_top), inv = 127.f * rcp;
+    };
+    if (EXACT) write_scale();
+    const float rcp = __frcp_rn(a32), inv = 127.f * rcp;
     int8_t* q_row = a.q + row * a.q_ld;
     // q of the group `v`; a bit for each that 64 bits have to decide
     auto quantise = [&](int v, Pair (&f)[4]) {
@@ -582,7 +598,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         if constexpr (DIVIDE) {
             // 127 p / a, rounded correctly (Markstein: a quotient from the reciprocal, its remainder by fma, one correction), and
             // that to an integer: a quotient between two halves keeps its side, a tie is exact (see DIVIDE)
-            const Pair r = pair(rcp, rcp), minus_a = pair(-a32_top, -a32_top);
+            const Pair r = pair(rcp, rcp), minus_a = pair(-a32, -a32);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float lo, hi;
@@ -625,6 +641,10 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if ((t + i * TPR) * 8 < a.h) open |= quantise(t + i * TPR, p[i]) << (8 * i);
+        if constexpr (!EXACT && TPR > 32) {
+            __syncthreads();
+            a64 = __longlong_as_double(static_cast<long long>(sc->top64));
+        }
         if constexpr (!DIVIDE) decide(open, t);
     } else {
         for (int base = t; base * 8 < a.h; base += NV * TPR)
@@ -633,6 +653,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
                 if constexpr (!DIVIDE) decide(open, v);
             });
     }
+    if (!EXACT) write_scale();
     }
     if (!set_aside) return;
     if constexpr (TPR > 32) __syncthreads();
