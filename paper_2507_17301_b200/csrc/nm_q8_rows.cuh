@@ -47,8 +47,21 @@ struct alignas(sizeof(T) * 8 < 16 ? sizeof(T) * 8 : 16) Eight {
     T v[8];
 };
 
-// Eight consecutive elements, the `n` first of which exist (zeros for the others); VEC: `p` is 16-byte aligned.
-template <typename T, bool VEC>
+// The columns of a group: eight consecutive ones where rows can be read 16 bytes at a time, else every TPR-th, so that neighbouring
+// threads read neighbouring columns (4096 x 1001 bf16 with eight consecutive ones everywhere 21.6 us).
+template <int TPR, bool VEC>
+struct Group {
+    int first, count;   // of them; may be more than eight, or none
+    static constexpr int step = VEC ? 1 : TPR;
+    __device__ __forceinline__ Group(int v, int h)
+    {
+        first = VEC ? v * 8 : v / TPR * 8 * TPR + v % TPR;
+        count = VEC ? h - first : (h - first + TPR - 1) / TPR;
+    }
+};
+
+// Eight elements `STEP` apart, the `n` first of which exist (zeros for the others); VEC: consecutive, and `p` is 16-byte aligned.
+template <typename T, bool VEC, int STEP>
 __device__ __forceinline__ Eight<T> load8(const T* p, int n)
 {
     Eight<T> e;
@@ -62,10 +75,10 @@ __device__ __forceinline__ Eight<T> load8(const T* p, int n)
         return e;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e.v[i] = i < n ? p[i] : from_float<T>(0.f);
+    for (int i = 0; i < 8; ++i) e.v[i] = i < n ? p[i * STEP] : from_float<T>(0.f);
     return e;
 }
-template <typename T, bool VEC>
+template <typename T, bool VEC, int STEP>
 __device__ __forceinline__ void store8(T* p, const Eight<T>& e, int n)
 {
     if (VEC && n >= 8) {
@@ -79,7 +92,7 @@ __device__ __forceinline__ void store8(T* p, const Eight<T>& e, int n)
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (i < n) p[i] = e.v[i];
+        if (i < n) p[i * STEP] = e.v[i];
 }
 
 // x + r, rounded once: for 16-bit types the two-way addition, which gives what a sum in 32 bits rounded to 16 gives (where that
@@ -292,36 +305,45 @@ __device__ __forceinline__ double row_max(double v, double* part)
 }
 
 // The whole row in 64 bits (its thread `t` of TPR; all of them come here together).
-template <Q8RowOp OP, typename T, typename W, int TPR>
+template <Q8RowOp OP, typename T, typename W, int TPR, bool VEC>
 __device__ __noinline__ void row_in_64(const Q8Rows& a, size_t row, int t, bool zero, Scratch* sc)
 {
+    using G = Group<TPR, VEC>;
     if (zero) {
         // every product is 0 in 32 bits: usually a row of padding.  It is one of zeros if every product has a factor 0
         int some = 0;
-        for (int v = t; v * 8 < a.h; v += TPR)
-            for (int c = v * 8; c < min(v * 8 + 8, a.h); ++c) some |= product_of_non_zeros<OP, T, W>(a, row, c);
+        for (int v = t;; v += TPR) {
+            const G g(v, a.h);
+            if (g.count <= 0) break;
+            for (int e = 0; e < min(g.count, 8); ++e) some |= product_of_non_zeros<OP, T, W>(a, row, g.first + e * G::step);
+        }
         if constexpr (TPR > 32) some = __syncthreads_or(some);
         else some = __any_sync(0xFFFFFFFFu, some);
         if (!some) {
             if (t == 0) a.scale[row] = 0.f;
-            for (int v = t; v * 8 < a.h; v += TPR) {
-                int8_t* q = a.q + row * a.q_ld + v * 8;
-                if (a.h - v * 8 >= 8) *reinterpret_cast<uint2*>(q) = make_uint2(0u, 0u);
-                else for (int c = 0; c < a.h - v * 8; ++c) q[c] = 0;
+            for (int v = t;; v += TPR) {
+                const G g(v, a.h);
+                if (g.count <= 0) break;
+                int8_t* q = a.q + row * a.q_ld + g.first;
+                if (VEC && g.count >= 8) *reinterpret_cast<uint2*>(q) = make_uint2(0u, 0u);
+                else for (int e = 0; e < min(g.count, 8); ++e) q[e * G::step] = 0;
             }
             return;
         }
     }
     double top = 0.0, sum = 0.0;
     int bad = 0;
-    for (int v = t; v * 8 < a.h; v += TPR)
-        for (int c = v * 8; c < min(v * 8 + 8, a.h); ++c) {
+    for (int v = t;; v += TPR) {
+        const G g(v, a.h);
+        if (g.count <= 0) break;
+        for (int e = 0; e < min(g.count, 8); ++e) {
             double s = 0.0;
-            const double p = exact_value<OP, T, W>(a, row, c, &s);
+            const double p = exact_value<OP, T, W>(a, row, g.first + e * G::step, &s);
             bad |= !(fabs(p) <= 1e300) || !(fabs(s) <= 1e300);
             top = fmax(top, fabs(p));
             sum += s * s;
         }
+    }
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
     bad = __any_sync(0xFFFFFFFFu, bad);
     if constexpr (TPR > 32) {
@@ -345,10 +367,15 @@ __device__ __noinline__ void row_in_64(const Q8Rows& a, size_t row, int t, bool 
     const float stored = static_cast<float>(scale);
     const bool good = !bad && stored < INFINITY;
     if (t == 0) a.scale[row] = good ? stored : NAN;
-    for (int v = t; v * 8 < a.h; v += TPR)
-        for (int c = v * 8; c < min(v * 8 + 8, a.h); ++c)
+    for (int v = t;; v += TPR) {
+        const G g(v, a.h);
+        if (g.count <= 0) break;
+        for (int e = 0; e < min(g.count, 8); ++e) {
+            const int c = g.first + e * G::step;
             a.q[row * a.q_ld + c] =
                 good && top > 0.0 ? static_cast<int8_t>(rint(127.0 * exact_value<OP, T, W>(a, row, c) / top)) : static_cast<int8_t>(0);
+        }
+    }
 }
 
 // TPR threads take a row, each NV groups of eight columns, in steps of TPR groups.  KEEP: the row's p stay in registers (8 * NV * TPR >= h).
@@ -365,6 +392,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     // is a multiple of p's last place, more than 2^-16 p, and that over 2 a is more than 2^-24 of the quotient
     constexpr bool DIVIDE = sizeof(T) == 2 && (OP == Q8_ROWS || (OP == Q8_RMSNORM && std::is_same_v<T, __nv_bfloat16> && sizeof(W) == 2));
     constexpr bool ASYNC = SLOTS > 0;
+    using G = Group<TPR, VEC>;
     static_assert(!ASYNC || (KEEP && VEC), "copied pieces are read once, 16 bytes at a time");
     extern __shared__ uint4 smem[];
     __shared__ Scratch scratch[2];   // rows take turns: a row's is written after the barrier behind the last reading of it
@@ -429,7 +457,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             Eight<T> es = ex;
             if (TWO && first) {
                 es = add8<T>(ex, er);
-                store8<T, VEC>(s_row + v * 8, es, a.h - v * 8);
+                const G g(v, a.h);
+                store8<T, VEC, G::step>(s_row + g.first, es, g.count);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -465,24 +494,27 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         Eight<T> ex[NV], er[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = base + i * TPR, n = a.h - v * 8;
-            if (n <= 0) continue;
+            const G g(base + i * TPR, a.h);
+            if (g.count <= 0) continue;
             // the second reading of a norm's row finds the sum in memory
             const T* from = OP == Q8_RMSNORM && TWO && !first ? s_row : x;
-            ex[i] = load8<T, VEC>(from + v * 8, n);
-            if (TWO && (OP == Q8_SILU_MUL || first)) er[i] = load8<T, VEC>(r + v * 8, n);
+            ex[i] = load8<T, VEC, G::step>(from + g.first, g.count);
+            if (TWO && (OP == Q8_SILU_MUL || first)) er[i] = load8<T, VEC, G::step>(r + g.first, g.count);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = base + i * TPR;
-            if (v * 8 >= a.h) continue;
+            const G g(v, a.h);
+            if (g.count <= 0) continue;
             Eight<W> ew;
-            if (OP == Q8_RMSNORM) ew = load8<W, VEC>(weight + v * 8, a.h - v * 8);   // (out of the L1: every row reads them)
+            if (OP == Q8_RMSNORM) ew = load8<W, VEC, G::step>(weight + g.first, g.count);   // (out of the L1: every row reads them)
             Pair tmp[4];
             values(v, tmp, ex[i], er[i], ew, first);
             use(i, v, tmp);
         }
     };
+    // groups of a row that is read again: this thread's `base`, base + NV * TPR, ...
+    auto begins = [&](int base) { return G(base, a.h).count > 0; };
     if constexpr (ASYNC) {
         if constexpr (SLOTS == 2) {
             if (row + step < tokens) fetch(row + step, turn ^ 1);
@@ -497,7 +529,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             Eight<T> er = {};
             Eight<W> ew = {};
             if (v * 8 >= a.h) continue;
-            if (OP == Q8_RMSNORM) ew = load8<W, VEC>(weight + v * 8, a.h - v * 8);   // (out of the L1: every row reads them)
+            if (OP == Q8_RMSNORM) ew = load8<W, VEC, 1>(weight + v * 8, a.h - v * 8);   // (out of the L1: every row reads them)
             if (TWO) er = fetched(turn, 1, i);
             values(v, p[i], fetched(turn, 0, i), er, ew, true);
         }
@@ -507,7 +539,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             for (int e = 0; e < 4; ++e) p[i][e] = f[e];
         });
     } else {
-        for (int base = t; base * 8 < a.h; base += NV * TPR) pass(base, true, [](int, int, Pair (&)[4]) {});
+        for (int base = t; begins(base); base += NV * TPR) pass(base, true, [](int, int, Pair (&)[4]) {});
     }
 
     float sum = 0.f;
@@ -543,6 +575,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         continue;
     }
     // (element `at` of this thread's part: group at / 8, column at % 8 of it)
+    auto column_of = [&](int v0, int at) { return G(v0 + at / 8 * TPR, a.h).first + at % 8 * G::step; };
     auto input_at = [&](int tensor, int at) {
         return ASYNC ? nmk::smem_u32(place(turn, TWO ? tensor : 0, at / 8, at % 8 / (8 / PIECES))) + static_cast<uint32_t>(at % (8 / PIECES) * sizeof(T)) : 0u;
     };
@@ -555,7 +588,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         auto look = [&](uint32_t bits, int v0) {
             for (; bits; bits &= bits - 1u) {
                 const int at = __ffs(bits) - 1;
-                mine = fmax(mine, again<OP, T, W>(a, row, (v0 + at / 8 * TPR) * 8 + at % 8, input_at(0, at), input_at(1, at), 0.0));
+                mine = fmax(mine, again<OP, T, W>(a, row, column_of(v0, at), input_at(0, at), input_at(1, at), 0.0));
             }
         };
         if (top < near_top) {
@@ -564,10 +597,10 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             uint32_t bits = 0u;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if ((t + i * TPR) * 8 < a.h) bits |= which(p[i], is_near) << (8 * i);
+                if (begins(t + i * TPR)) bits |= which(p[i], is_near) << (8 * i);
             look(bits, t);
         } else {
-            for (int base = t; base * 8 < a.h; base += NV * TPR)
+            for (int base = t; begins(base); base += NV * TPR)
                 pass(base, false, [&](int, int v, Pair (&f)[4]) { look(which(f, is_near), v); });
         }
         // The maximum in 64 bits decides only where 32 leave a quotient open: it is collected while all threads go on with the one in 32
@@ -619,11 +652,13 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         }
         const uint32_t lo = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
         const uint32_t hi = __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410);
-        const int n = a.h - v * 8;
-        if (n >= 8) {
-            *reinterpret_cast<uint2*>(q_row + v * 8) = make_uint2(lo, hi);
+        const G g(v, a.h);
+        if (VEC && g.count >= 8) {
+            *reinterpret_cast<uint2*>(q_row + g.first) = make_uint2(lo, hi);
         } else {
-            for (int e = 0; e < n; ++e) q_row[v * 8 + e] = static_cast<int8_t>((e < 4 ? lo >> (8 * e) : hi >> (8 * (e - 4))) & 0xFFu);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < g.count) q_row[g.first + e * G::step] = static_cast<int8_t>((e < 4 ? lo >> (8 * e) : hi >> (8 * (e - 4))) & 0xFFu);
         }
         return border > kBorder ? which(f, [&](float p) {
             uint32_t unused;
@@ -632,7 +667,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     };
     auto decide = [&](uint32_t bits, int v0) {
         for (; bits; bits &= bits - 1u) {
-            const int at = __ffs(bits) - 1, col = (v0 + at / 8 * TPR) * 8 + at % 8;
+            const int at = __ffs(bits) - 1, col = column_of(v0, at);
             if (col < a.h) again<OP, T, W>(a, row, col, input_at(0, at), input_at(1, at), a64);
         }
     };
@@ -640,14 +675,14 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         uint32_t open = 0u;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if ((t + i * TPR) * 8 < a.h) open |= quantise(t + i * TPR, p[i]) << (8 * i);
+            if (begins(t + i * TPR)) open |= quantise(t + i * TPR, p[i]) << (8 * i);
         if constexpr (!EXACT && TPR > 32) {
             __syncthreads();
             a64 = __longlong_as_double(static_cast<long long>(sc->top64));
         }
         if constexpr (!DIVIDE) decide(open, t);
     } else {
-        for (int base = t; base * 8 < a.h; base += NV * TPR)
+        for (int base = t; begins(base); base += NV * TPR)
             pass(base, false, [&](int, int v, Pair (&f)[4]) {
                 const uint32_t open = quantise(v, f);
                 if constexpr (!DIVIDE) decide(open, v);
@@ -662,7 +697,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         const float mark = *reinterpret_cast<volatile float*>(a.scale + row);
         if constexpr (TPR > 32) __syncthreads();   // (its first thread replaces the mark, and the scratch is used again)
         else __syncwarp();
-        if (mark < 0.f) row_in_64<OP, T, W, TPR>(a, row, t, mark == -2.f, scratch);
+        if (mark < 0.f) row_in_64<OP, T, W, TPR, VEC>(a, row, t, mark == -2.f, scratch);
     }
 }
 
@@ -682,17 +717,22 @@ cudaError_t launch_one(const Q8Rows& a, cudaStream_t st)
     return nmhost::launch_pdl(kernel, static_cast<unsigned>(blocks < resident ? blocks : resident), static_cast<unsigned>(threads), smem, st, a);
 }
 
-// Threads for a row, four groups of eight columns each (two of 32-bit numbers); fewer groups where there are too few rows to fill the GPU.
+// Threads for a row, four groups of eight columns each (two of 32-bit numbers); fewer groups, of more threads, where there are too few rows
+// to fill the GPU: 333 x 1001 fp32 (rows off the 16-byte boundaries) a block of 256 to a row 3.2 us, a warp 7.8; 4096 x 1001 bf16 21 and 16.5.
 template <Q8RowOp OP, bool TWO, typename T, typename W>
 cudaError_t launch_shape(const Q8Rows& a, bool vec, cudaStream_t st)
 {
 #define NM_ROWS(TPR, NV, KEEP, VEC, SLOTS) launch_one<OP, TWO, T, W, TPR, NV, KEEP, VEC, SLOTS>(a, st)
+    const bool few = a.tokens <= 2 * nmhost::sm_count();
     if (!vec) {
         if (a.h <= 512) return NM_ROWS(32, 2, true, false, 0);
-        if (a.h <= 4096) return NM_ROWS(256, 2, true, false, 0);
+        if (a.h <= 4096 && a.tokens <= 6 * nmhost::sm_count()) return NM_ROWS(256, 2, true, false, 0);
+        if (a.h <= 1024) return NM_ROWS(32, 4, true, false, 0);
+        if (a.h <= 4096) return NM_ROWS(128, 4, true, false, 0);
+        if (a.h <= 8192) return NM_ROWS(256, 4, true, false, 0);
+        if (a.h <= 16384) return NM_ROWS(512, 4, true, false, 0);
         return NM_ROWS(512, 2, false, false, 0);
     }
-    const bool few = a.tokens <= 2 * nmhost::sm_count();
     if (a.h <= 512) return NM_ROWS(32, 2, true, true, 2);
     if (a.h <= 2048 && !few) return NM_ROWS(128, 2, true, true, 2);
     if (few) {
@@ -702,6 +742,7 @@ cudaError_t launch_shape(const Q8Rows& a, bool vec, cudaStream_t st)
     if constexpr (sizeof(T) == 4) {
         if (a.h <= 4096) return NM_ROWS(256, 2, true, true, 2);
         if (a.h <= 8192) return NM_ROWS(512, 2, true, true, 2);
+        if (a.h <= 12288) return NM_ROWS(768, 2, true, true, 2);
         if (a.h <= 16384) return NM_ROWS(1024, 2, true, true, 1);
     } else {
         if (few && a.h <= 16384) return NM_ROWS(1024, 2, true, true, 2);
