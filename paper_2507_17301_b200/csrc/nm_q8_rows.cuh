@@ -709,7 +709,7 @@ cudaError_t launch_one(const Q8Rows& a, cudaStream_t st)
     // as many blocks as an SM holds for certain (768 threads, 227 KB)
     constexpr size_t smem = static_cast<size_t>(threads) * NV * 8 * sizeof(T) * SLOTS * (TWO ? 2 : 1);
     int resident = threads > 768 ? 1 : 768 / threads;
-    if (smem && 225 * 1024 / (smem + 3072) < static_cast<size_t>(resident)) resident = static_cast<int>(225 * 1024 / (smem + 3072));
+    if (smem && 225 * 1024 / (smem + 3 * 1024) < static_cast<size_t>(resident)) resident = static_cast<int>(225 * 1024 / (smem + 3 * 1024));
     resident *= nmhost::sm_count();
     auto kernel = k_q8_rows<OP, TWO, T, W, TPR, NV, KEEP, VEC, SLOTS>;
     const cudaError_t e = nmhost::ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);

@@ -369,3 +369,27 @@ def test_pruning_rules_of_four_columns(nm):
         x, xs = activations(tokens, k)
         y = nm.nm_q8_linear(h, on_gpu(x), torch.from_numpy(xs).cuda(), out_dtype=torch.float32)
         check(y, x, xs, ref.dense_of(v, i, k, 16), s, None, torch.float32)
+
+
+@pytest.mark.parametrize("tokens,x_ld,y_ld,c_out", [(3, 2 ** 31 + 64, 2 ** 30 + 4, 130), (40, 2 ** 27, 2 ** 26 + 1, 130), (1100, 2 ** 22 + 16, 2 ** 21 + 4, 2200)])
+def test_offsets_past_32_bits(nm, tokens, x_ld, y_ld, c_out):
+    """Rows of activations and outputs gigabytes apart, in each kernel, and rows of the operators that make them."""
+    k = 520
+    v, s, i = layer(c_out, k, 2, 4, 32)
+    h = import_layer(nm, v, s, i, k, 2, 4, 32)
+    x, xs = activations(tokens, k)
+    xb = torch.zeros((tokens - 1) * x_ld + 1024, dtype=torch.int8, device="cuda")
+    yb = torch.zeros((tokens - 1) * y_ld + 4096, dtype=torch.float32, device="cuda")
+    xg, y = xb.as_strided((tokens, k), (x_ld, 1)), yb.as_strided((tokens, c_out), (y_ld, 1))
+    xg.copy_(torch.from_numpy(x))
+    nm.nm_q8_linear(h, xg, torch.from_numpy(xs).cuda(), y=y)
+    nm.nm_q8_weights_check(h)
+    check(y, x, xs, ref.dense_of(v, i, k, 32), s, None, torch.float32)
+    a = yb.as_strided((tokens, k), (y_ld, 1))
+    a.copy_(torch.randn(tokens, k, generator=torch.Generator().manual_seed(3)))
+    q, scale = nm.nm_q8_rows(a, q=xg)
+    assert q.data_ptr() == xg.data_ptr() and torch.equal(q.cpu(), ref.rows(a.cpu())[0])
+    w = torch.randn(k, generator=torch.Generator().manual_seed(4))
+    want_q, _, want_r = ref.rmsnorm(a.cpu(), w, 1e-6, a.cpu())
+    q, scale, r = nm.nm_q8_rmsnorm(a, w.cuda(), 1e-6, residual=a, residual_out=a, q=xg)
+    assert torch.equal(r.cpu(), want_r) and torch.equal(q.cpu(), want_q)
