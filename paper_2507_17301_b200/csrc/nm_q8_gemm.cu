@@ -1,14 +1,16 @@
 // Product of 8-bit activations with column-wise N:M pruned 8-bit weights on the tensor core (kind::i8, exact 32-bit sums).
 //
-//   D[channel][token] = sum over 128-column blocks of  W[128 channels x 128] * X[BN tokens x 128]^T
+//   D[channel][token] = sum over blocks of columns of  W[128 channels x block] * X[BN tokens x block]^T
 //
-// Weights are the M side (128 channels a tile), tokens the N side (16 to 256), so that a few tokens fill an instruction as well as
-// many.  Pruned columns are zeros of the expanded weights: the 16 KB of a tile and block lie in memory as the swizzled
-// shared-memory image, one bulk copy; activations come by TMA, zeros past the last column and token.
-// Where there are far fewer tiles than SMs the reduction axis is split over the 2, 4 or 8 CTAs of a cluster: each sends the runs of tokens
+// Weights are the M side (128 channels a tile), tokens the N side (16 to 128), so that a few tokens fill an instruction as well as
+// many.  A block is 128 columns of the expanded weights, whose pruned columns are zeros, or, where a pattern keeps at most two of
+// four aligned columns, 256 columns of the sparse form: the same 16 KB and 4 KB of places, which go to tensor memory, for the sparse
+// instruction.  Either lies in memory as the shared-memory image, one bulk copy; activations come by TMA, zeros past the last
+// column and token.
+// Where there are far fewer tiles than SMs the reduction axis is split over the 2 or 4 CTAs of a cluster: each sends the runs of tokens
 // that another finishes as one bulk copy into that CTA's shared memory.  Sums are integers: the result does not depend on the split.
 //
-//   producer (1 thread), MMA issuer (1 thread), epilogue (4 warps, a lane per channel): y = (sum * x_scale) * w_scale + bias
+//   producer (1 thread), MMA issuer (1 thread), epilogue (4 warps): sums through shared memory to rows of tokens, y = (sum * x_scale) * w_scale + bias
 #include <algorithm>
 
 #include <cuda_bf16.h>
@@ -25,6 +27,7 @@ using namespace nmk;
 constexpr int THREADS = 192;   // warps: 0 producer, 1 MMA issuer and tensor memory, 2-5 epilogue
 constexpr int NSTAGE_MAX = 8;
 constexpr int A_BYTES = 128 * 128;
+constexpr int MOST_TOKENS = 128;   // of a tile; more than a round of such tiles is the pair kernel's
 constexpr int PLACES = 4096;   // bytes of a sparse stage's places
 
 struct GemmArgs {
@@ -87,7 +90,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
     __shared__ uint64_t s_full[NSTAGE_MAX], s_free[NSTAGE_MAX], s_acc, s_recv;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
-    __shared__ float s_scale[256];   // of the tile's tokens
+    __shared__ float s_scale[MOST_TOKENS];   // of the tile's tokens
 
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
     const uint32_t rank = g.ks > 1 ? cluster_ctarank() : 0u;
@@ -291,23 +294,22 @@ nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
     g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows;
     g.blocks = sparse ? w->s_blocks : w->k_blocks;
     g.c_tiles = (w->c_out + 127) / 128;
-    // The narrowest tiles that still are one round, us: 4096 -> 4096, 128 tokens in tiles of 16 / 32 / 64 / 128: 16.0 / 8.7 / 9.2 / 11.1; 512 tokens:
-    // 56 / 34 / 19 / 12.2.  A split of the reduction axis pays where half the SMs would idle (16 tokens, 2048 -> 2048: 5.0 whole, 3.8 in
-    // four), not in eight (7.9).
-    g.bn = 16;
-    auto items_of = [&](int bn) { return static_cast<long long>(g.c_tiles) * ((p.tokens + bn - 1) / bn); };
-    while (g.bn < 256 && g.bn < p.tokens && items_of(g.bn) > sm_count()) g.bn *= 2;
-    const long long items = items_of(g.bn);
+    // The narrowest tiles (in sixteens) that still are one round, us: 4096 -> 4096, 128 tokens in tiles of 16 / 32 / 64 / 128: 16.0 / 8.7 / 9.2 /
+    // 11.1; 512 tokens: 56 / 34 / 19 / 12.2.  A split of the reduction axis pays where half the SMs would idle (16 tokens, 2048 -> 2048: 5.0
+    // whole, 3.8 in four), not in eight (7.9).  (Figures of dense weights.)
+    const int columns = std::max(1, sm_count() / g.c_tiles);   // tiles along the tokens
+    g.bn = static_cast<int>(std::min<long long>(MOST_TOKENS, ((static_cast<long long>(p.tokens) + columns - 1) / columns + 15) / 16 * 16));
+    const long long items = static_cast<long long>(g.c_tiles) * ((p.tokens + g.bn - 1) / g.bn);
     if (items > (1ll << 27)) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: too many tiles");
     g.ks = 1;
-    while (g.bn <= 128 && g.ks < 4 && items * g.ks * 2 <= sm_count() && g.blocks * (sparse ? 2 : 1) >= g.ks * 4) g.ks *= 2;
+    while (g.ks < 4 && items * g.ks * 2 <= sm_count() && g.blocks * (sparse ? 2 : 1) >= g.ks * 4) g.ks *= 2;
     // More than a round of CTAs: two on an SM, one sets up and loads while the other finishes (in one round the deeper ring is faster:
     // 4096 -> 4096, 512 tokens 12.2 us against 16.9)
-    const bool half = g.bn <= 128 && items > sm_count();
+    const bool half = items > sm_count();
     g.stage_bytes = sparse ? A_BYTES + PLACES + 2 * g.bn * 128 : A_BYTES + g.bn * 128;
     const int budget = (half ? 112 : 224) * 1024 - 1024 - 2048 - (g.ks > 1 ? g.bn * 512 : 0);
     g.stages = std::min(NSTAGE_MAX, budget / g.stage_bytes);
-    // (the sums of a tile, bn * 512 bytes, go through the ring, which has at least 96 KB, 168 KB with bn = 256)
+    // (the sums of a tile, bn * 512 bytes, at most 64 KB, go through the ring, which has at least 96 KB)
     g.tmem = 32;
     while (g.tmem < g.bn + (sparse ? 8 * g.stages : 0)) g.tmem *= 2;
     alignas(64) CUtensorMap tm;

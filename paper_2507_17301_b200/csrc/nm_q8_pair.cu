@@ -2,11 +2,15 @@
 //
 //   D[256 channels][256 tokens] += W[256 x 128] * X[256 x 128]^T   a stage
 //
-// Weights are the expanded form (pruned columns are zeros), the M side of the instruction; tokens are the N side.  A pair's MMA is 256 x
+// Weights are the M side of the instruction, tokens the N side.  In the expanded form (pruned columns are zeros):  A pair's MMA is 256 x
 // 256 x 32: each CTA holds the weights of its own 128 channels and the activations of HALF the tokens (the hardware exchanges the
 // halves), so that a stage of 128 columns is 32 KB written to and 32 KB read from a CTA's shared memory for 512 tensor cycles; a CTA by
 // itself would need 48 KB of each, which is more than shared memory moves in that time.  Sums of a CTA's channels stay in its own tensor
 // memory, two tiles of 256 columns in turn, so that one is written out while the next is added up.
+// In the sparse form (patterns that keep at most two of four aligned columns) a stage is 256 columns, 16 KB of weights, 4 KB of their places,
+// which go to tensor memory ahead of the MMAs, and 28 KB of activations: 224 tokens a tile, so that the places of four stages fit beside
+// the sums.  4096 -> 12288 at 2:4, 8192 tokens: 242 us expanded, 184 sparse (2.2 POP/s on the retained weights): 92 KB through shared
+// memory a stage, 720 cycles, against 448 tensor cycles.
 //
 //   producer (1 thread per CTA)   a bulk copy of the weights' swizzled image and a TMA load of the activations per stage
 //   relay (1 thread, second CTA)  forwards "stage landed" to the first CTA's barrier
@@ -329,9 +333,9 @@ namespace nmhost {
 
 bool q8_pair_takes(const Q8Linear& p)
 {
-    // One round of the other kernel's tiles of 128 x 128 or less is faster, us (this / the other): 4096 -> 4096, 512 tokens 16.2 / 12.2, 768
-    // tokens 17.0 / 19.8; 2048 -> 2048, 1024 tokens 11.7 / 9.1, 2048 tokens 12.8 / 15.0; 4096 -> 12288, 128 tokens 15.3 / 14.1, 200 tokens
-    // 16.6 / 19.9.
+    // One round of the other kernel's tiles of 128 x 128 or less is faster, us (this / the other) at 2:4: 4096 -> 4096, 512 tokens 12.5 / 11.6, 640
+    // tokens 12.6 / 20.0; 2048 -> 2048, 1024 tokens 9.5 / 8.9, 1500 tokens 10.1 / 14.5; 4096 -> 12288, 96 tokens 11.7 / 11.7, 160 tokens
+    // 12.9 / 19.2; 4096 -> 1001, 2048 tokens 15.7 / 12.3.
     const long long small = static_cast<long long>((p.w->c_out + 127) / 128) * ((static_cast<long long>(p.tokens) + 127) / 128);
     const long long work = static_cast<long long>(p.w->rows / 256) * ((static_cast<long long>(p.tokens) + 223) / 224);
     return p.tokens > 128 && small > sm_count() && work < (1ll << 30) && max_pairs() > 0;

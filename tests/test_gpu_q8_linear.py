@@ -393,3 +393,22 @@ def test_offsets_past_32_bits(nm, tokens, x_ld, y_ld, c_out):
     want_q, _, want_r = ref.rmsnorm(a.cpu(), w, 1e-6, a.cpu())
     q, scale, r = nm.nm_q8_rmsnorm(a, w.cuda(), 1e-6, residual=a, residual_out=a, q=xg)
     assert torch.equal(r.cpu(), want_r) and torch.equal(q.cpu(), want_q)
+
+
+@pytest.mark.parametrize("c_out,tokens", [(4096, 9), (4096, 100), (4096, 333), (4096, 512), (12288, 20), (12288, 61), (12288, 128), (20000, 11), (20000, 77), (20000, 128),
+                                          (1100, 640), (700, 30), (2200, 40)])
+@pytest.mark.parametrize("k,n,m", [(700, 2, 4), (1300, 4, 4)])
+def test_middling_tokens(nm, c_out, tokens, k, n, m):
+    """Tiles of 16 to 128 tokens, split and whole, one round of them and more, sparse and dense."""
+    v, s, i = layer(c_out, k, n, m, 64, seed=3)
+    h = import_layer(nm, v, s, i, k, n, m, 64)
+    x, xs = activations(tokens, k)
+    dense = torch.from_numpy(ref.dense_of(v, i, k, 64)).cuda()
+    prod = (torch.from_numpy(x).cuda().double() @ dense.T) * torch.from_numpy(xs).cuda().double()[:, None] * torch.from_numpy(s).cuda().double()
+    buf = torch.full((tokens + 1, c_out), 5.0, device="cuda")
+    y = nm.nm_q8_linear(h, on_gpu(x), torch.from_numpy(xs).cuda(), y=buf[:tokens])
+    nm.nm_q8_weights_check(h)
+    assert torch.all((y.double() - prod).abs() <= prod.abs() * 3.1 * 2.0 ** -24 + 2.0 ** -126)
+    assert torch.all(buf[tokens] == 5.0)
+    half = nm.nm_q8_linear(h, on_gpu(x), torch.from_numpy(xs).cuda(), out_dtype=torch.bfloat16)
+    assert torch.all((half.double() - prod).abs() <= prod.abs() * (2.0 ** -8 + 2.0 ** -20) + 2.0 ** -126)
