@@ -13,8 +13,8 @@
 // are done in 64 bits altogether: zeros give q = 0 and scale 0, a row that is not finite gives q = 0 and scale NaN.
 //
 // Each element is read and written once.  Persistent blocks: a thread has its part of the next row on its way to shared memory (16 bytes a
-// copy, places of its own, no barrier) while the row before is reduced and written.  8192 x 8192 bf16 with residual 89.5 us, 80 % of the
-// copy rate; gated 4096 x 12288 bf16 66 us, 58 %, bound by instruction issue; rows that do not start on 16 bytes go without the copies.
+// copy, places of its own, no barrier) while the row before is reduced and written.  8192 x 8192 bf16 with residual 86.5 us, 83 % of the
+// copy rate; gated 4096 x 12288 bf16 63 us, 61 %, bound by instruction issue; rows that do not start on 16 bytes go without the copies.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -410,21 +410,22 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
     auto place = [&](int turn, int tensor, int i, int piece) {
         return places + (((SLOTS == 2 ? turn : 0) * (TWO ? 2 : 1) + tensor) * NV * PIECES + i * PIECES + piece) * THREADS;
     };
+    const int left = a.h - t * 8;   // columns from this thread's first group on
     auto fetch = [&](size_t row, int turn) {
-        const T* x = static_cast<const T*>(a.x) + row * a.x_ld;
-        const T* r = static_cast<const T*>(a.r) + row * a.r_ld;
+        const T* x = static_cast<const T*>(a.x) + row * a.x_ld + t * 8;
+        const T* r = static_cast<const T*>(a.r) + (TWO ? row * a.r_ld + t * 8 : 0);
+        const uint32_t to = nmk::smem_u32(place(turn, 0, 0, 0));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = t + i * TPR;
-            if (v * 8 >= a.h) continue;
+            if (left <= i * TPR * 8) continue;
 #pragma unroll
             for (int piece = 0; piece < PIECES; ++piece) {
                 // zeros behind the last column (of a group of fp32 numbers the second piece may be all behind it: nothing is read then)
-                const int bytes = (a.h - v * 8) * static_cast<int>(sizeof(T)) - piece * 16;
-                const uint32_t some = bytes < 16 ? (bytes > 0 ? bytes : 0) : 16;
-                const int from = some ? v * 8 + piece * (16 / static_cast<int>(sizeof(T))) : 0;
-                nmk::cp_async16(nmk::smem_u32(place(turn, 0, i, piece)), x + from, some);
-                if (TWO) nmk::cp_async16(nmk::smem_u32(place(turn, 1, i, piece)), r + from, some);
+                const int bytes = (left - i * TPR * 8) * static_cast<int>(sizeof(T)) - piece * 16;
+                const uint32_t some = PIECES == 1 ? min(bytes, 16) : max(min(bytes, 16), 0);
+                const int from = PIECES == 1 || some ? i * TPR * 8 + piece * (16 / static_cast<int>(sizeof(T))) : 0;
+                nmk::cp_async16(to + (i * PIECES + piece) * THREADS * 16, x + from, some);
+                if (TWO) nmk::cp_async16(to + ((NV + i) * PIECES + piece) * THREADS * 16, r + from, some);
             }
         }
     };
@@ -436,6 +437,14 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         }
         return e;
     };
+    // 16-bit weights stay in registers from row to row
+    constexpr bool HELD = ASYNC && OP == Q8_RMSNORM && sizeof(W) == 2 && TPR < 1024;
+    Eight<W> held[HELD ? NV : 1];
+    if constexpr (HELD) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (left > i * TPR * 8) held[i] = load8<W, VEC, 1>(weight + t * 8 + i * TPR * 8, left - i * TPR * 8);
+    }
     // (whole rows leave: ROWS > 1 has no barrier across warps)
     size_t row = static_cast<size_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
     if constexpr (SLOTS == 2) {
@@ -527,13 +536,13 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
         nmk::cp_async_wait<SLOTS - 1>();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = t + i * TPR;
             Eight<T> er = {};
             Eight<W> ew = {};
-            if (v * 8 >= a.h) continue;
-            if (OP == Q8_RMSNORM) ew = load8<W, VEC, 1>(weight + v * 8, a.h - v * 8);   // (out of the L1: every row reads them)
+            if (left <= i * TPR * 8) continue;
+            if (HELD) ew = held[HELD ? i : 0];
+            else if (OP == Q8_RMSNORM) ew = load8<W, VEC, 1>(weight + t * 8 + i * TPR * 8, left - i * TPR * 8);   // (out of the L1: every row reads them)
             if (TWO) er = fetched(turn, 1, i);
-            values(v, p[i], fetched(turn, 0, i), er, ew, true);
+            values(t + i * TPR, p[i], fetched(turn, 0, i), er, ew, true);
         }
     } else if constexpr (KEEP) {
         pass(t, true, [&](int i, int, Pair (&f)[4]) {
