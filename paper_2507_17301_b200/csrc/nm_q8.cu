@@ -204,16 +204,16 @@ __global__ void __launch_bounds__(256) k_q8_sparse(const nm_q8_weights h)
     *reinterpret_cast<uint32_t*>(to + r % 128 / 8 * 256 + eighth / 4 * 128 + r % 8 * 16 + eighth % 4 * 4) = places;
 }
 
-// Most columns that an N:M pattern can keep of four aligned ones.
-int most_of_four(int n_keep, int m_group)
+// Most columns that an N:M pattern can keep of four aligned ones of k.
+int most_of_four(int n_keep, int m_group, int k)
 {
     int most = 0;
-    for (int i = 0; i < m_group; ++i) {   // (the pattern repeats after m_group fours)
+    for (int i = 0; i < m_group && 4 * i < k; ++i) {   // (the pattern repeats after m_group fours)
         int kept = 0;
         for (int c = 4 * i, end = 4 * i + 4; c < end;) {
-            const int stop = std::min(end, (c / m_group + 1) * m_group);
-            kept += std::min(n_keep, stop - c);
-            c = stop;
+            const int in_group = std::min(m_group - c % m_group, end - c);
+            kept += std::min(n_keep, in_group);
+            c += in_group;
         }
         most = std::max(most, kept);
     }
@@ -274,7 +274,7 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
     h->n_tiles = (c_out + tile_t - 1) / tile_t;
     h->k_blocks = (k + 127) / 128;
     h->rows = (c_out + 255) / 256 * 256;
-    if (most_of_four(n_keep, m_group) <= 2) h->s_blocks = (k + 255) / 256;
+    if (most_of_four(n_keep, m_group, k) <= 2) h->s_blocks = (k + 255) / 256;
     if (packed_tile(*h) >= 8) h->units = (packed_tile(*h) + 7) / 8;
     size_t total = 0;
     auto place = [&total](size_t bytes) {

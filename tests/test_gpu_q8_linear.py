@@ -412,3 +412,20 @@ def test_middling_tokens(nm, c_out, tokens, k, n, m):
     assert torch.all(buf[tokens] == 5.0)
     half = nm.nm_q8_linear(h, on_gpu(x), torch.from_numpy(xs).cuda(), out_dtype=torch.bfloat16)
     assert torch.all((half.double() - prod).abs() <= prod.abs() * (2.0 ** -8 + 2.0 ** -20) + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("n,m", [(2, 2 ** 31 - 1), (24, 2 ** 31 - 1), (2 ** 31 - 1, 2 ** 31 - 1), (2, 2 ** 30 + 1)])
+def test_groups_longer_than_a_row(nm, n, m):
+    # one group, of the k columns that exist
+    k, c_out = 100, 48
+    w = torch.randn(c_out, k, generator=torch.Generator().manual_seed(5)).cuda()
+    far, near = nm.nm_q8_prune(w, n, m, 16), nm.nm_q8_prune(w, min(n, k), k, 16)
+    v, s, i = nm.nm_q8_weights_export(far)
+    for got, want in zip((v, s, i), nm.nm_q8_weights_export(near)):
+        assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+    again = nm.nm_q8_weights_import(v, s, i, k, n, m, 16)
+    for tokens in (1, 20):
+        x, xs = nm.nm_q8_rows(torch.randn(tokens, k, generator=torch.Generator().manual_seed(tokens)).cuda())
+        want = nm.nm_q8_linear(near, x, xs, out_dtype=torch.float32)
+        assert torch.equal(nm.nm_q8_linear(far, x, xs, out_dtype=torch.float32), want)
+        assert torch.equal(nm.nm_q8_linear(again, x, xs, out_dtype=torch.float32), want)
