@@ -9,8 +9,10 @@
 // memory, two tiles of 256 columns in turn, so that one is written out while the next is added up.
 // In the sparse form (patterns that keep at most two of four aligned columns) a stage is 256 columns, 16 KB of weights, 4 KB of their places,
 // which go to tensor memory ahead of the MMAs, and 28 KB of activations: 224 tokens a tile, so that the places of four stages fit beside
-// the sums.  4096 -> 12288 at 2:4, 8192 tokens: 242 us expanded, 184 sparse (2.2 POP/s on the retained weights): 92 KB through shared
-// memory a stage, 720 cycles, against 448 tensor cycles.
+// the sums.  4096 -> 12288 at 2:4, 8192 tokens: 242 us expanded, 184 sparse (2.2 POP/s on the retained weights).  A stage takes 690 cycles,
+// not the 448 of the sparse rate: without the loads of activations it still takes 605 (480 with 128 tokens a tile, 570 with 192: about
+// 75 cycles an instruction whatever its width), and the copy of the places is no more than 10 of them.  Stages of the expanded form take
+// 520 of 512.
 //
 //   producer (1 thread per CTA)   a bulk copy of the weights' swizzled image and a TMA load of the activations per stage
 //   relay (1 thread, second CTA)  forwards "stage landed" to the first CTA's barrier
