@@ -169,8 +169,11 @@ constexpr float kError = OP == Q8_SILU_MUL ? 1.5e-5f : 4e-7f;
 constexpr float kMostProduct = 0x1p40f, kLeastTop = 0x1p-60f;
 constexpr float kMostTop = 0x1p100f;   // (127 p and 1 / a stay normal numbers)
 constexpr float kMostSum = 0x1p120f;
-// How near 127 p / a may come to a border between two integers, beside its own error, before 64 bits decide.
-constexpr float kBorder = 0.5f - 1e-7f;
+// How near 127 p / a may come to a border between two integers before 64 bits decide.  Its error is that of p and that of the maximum, both
+// relative to the quotient, which is up to a half more than the integer: border_of counts the integer's share, and the half's stands
+// here (all there is where the integer is 0), beside the roundings of 127 / a.
+template <Q8RowOp OP>
+constexpr float kBorder = 0.5f - kError<OP> - 1e-7f;
 
 // The products g u and g u / (1 + exp(-g)): (g u) first, whose underflow cannot matter beside kLeastTop.  Where the exponential
 // or its reciprocal leaves 32 bits (g < -87) the result is 0.  (Making good the exponent's rounding leaves a twentieth of the quotients
@@ -232,7 +235,7 @@ __device__ __forceinline__ bool product_of_non_zeros(const Q8Rows& a, size_t row
 
 constexpr float kRound = 12582912.f;   // adding 1.5 * 2^23 rounds to an integer, whose low byte is then the sum's
 
-// Distance of p * inv to the nearest integer plus what its error may add; the low byte of *k is the integer's.
+// Distance of p * inv to the nearest integer plus the error that goes with the integer (see kBorder); the low byte of *k is the integer's.
 template <Q8RowOp OP>
 __device__ __forceinline__ float border_of(float p, float inv, uint32_t* k)
 {
@@ -671,9 +674,9 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR < 128 ? 6 : TPR > 7
             for (int e = 0; e < 8; ++e)
                 if (e < g.count) q_row[g.first + e * G::step] = static_cast<int8_t>((e < 4 ? lo >> (8 * e) : hi >> (8 * (e - 4))) & 0xFFu);
         }
-        return border > kBorder ? which(f, [&](float p) {
+        return border > kBorder<OP> ? which(f, [&](float p) {
             uint32_t unused;
-            return border_of<OP>(p, inv, &unused) > kBorder;
+            return border_of<OP>(p, inv, &unused) > kBorder<OP>;
         }) : 0u;
     };
     auto decide = [&](uint32_t bits, int v0) {
