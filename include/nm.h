@@ -474,6 +474,15 @@ nm_status_t nm_autotune_tile(const float* w_dense, int c_out, int kh, int kw, in
 nm_status_t nm_selftest_wait_expiry(const nm_weights_t* w, void* cuda_stream);
 
 /*
+ * The same of the 8-bit product: nm_q8_linear's kernel of middling token counts (fp32 outputs, no bias) in which
+ * nothing is loaded from `block` of the reduction axis on (128 columns of it; 256 where the pattern keeps at most two of four aligned
+ * columns), so that the wait for it expires, after some seconds.  y is left as it was, nm_q8_weights_check(w) reports NM_ERR_TIMEOUT
+ * once, and the handle and the context stay usable.  A block past the last one: the product as it is.
+ */
+nm_status_t nm_selftest_q8_wait_expiry(const nm_q8_weights_t* w, const int8_t* x, long long x_ld, const float* x_scale, int tokens,
+                                       float* y, long long y_ld, int block, void* cuda_stream);
+
+/*
  * Plan cache: a text file with one line per layer, "<key> variant bn stages split kblk loads issuers ksplit"
  * (the analogue of keeping the profiler's choice per operator, Sec. 3.3; the last line of a key wins).
  *   nm_plan_key           writes the key of a layer (its geometry, pattern and tile width, batch and image size,

@@ -344,6 +344,39 @@ nm_status_t finish(const char* who, nm_q8_weights* h, const int8_t* values, cons
 
 }  // namespace
 
+// nm_q8_linear, and its self-test (never_loaded >= 0), whose calls all go to the kernel of middling token counts.
+static nm_status_t linear(const char* who, const nm_q8_weights_t* w, const int8_t* x, long long x_ld, const float* x_scale, int tokens, const float* bias,
+                          void* y, long long y_ld, nm_dtype_t y_dtype, int never_loaded, void* cuda_stream)
+{
+    if (!valid(w)) return fail(NM_ERR_INVALID_ARG, "%s: bad weights handle", who);
+    if (!known(y_dtype)) return fail(NM_ERR_INVALID_ARG, "%s: unknown type", who);
+    if (tokens < 0) return fail(NM_ERR_INVALID_ARG, "%s: tokens must be >= 0", who);
+    if (tokens > kMostTokens) return fail(NM_ERR_UNSUPPORTED, "%s: more than 2^30 tokens", who);
+    if (tokens == 0) return NM_OK;
+    if (!x || !x_scale || !y) return fail(NM_ERR_INVALID_ARG, "%s: x, x_scale or y is NULL", who);
+    if (tokens == 1) {
+        x_ld = (w->k + 15) / 16 * 16;
+        y_ld = w->c_out;
+    }
+    if (x_ld < w->k || y_ld < w->c_out) return fail(NM_ERR_INVALID_ARG, "%s: rows are closer than their length", who);
+    if (x_ld > (1ll << 38)) return fail(NM_ERR_UNSUPPORTED, "%s: rows of x are too far apart", who);
+    if (at(x) % 16 || x_ld % 16) return fail(NM_ERR_INVALID_ARG, "%s: x must be 16-byte aligned with rows a multiple of 16 bytes apart", who);
+    if (at(y) % size_of(y_dtype) || at(x_scale) % 4 || at(bias) % 4)
+        return fail(NM_ERR_INVALID_ARG, "%s: a tensor is not aligned to its elements", who);
+    const Span ys = {y, y_ld, w->c_out, size_of(y_dtype)}, all = {y, 0, (tokens - 1) * y_ld + w->c_out, size_of(y_dtype)};
+    if (overlap(ys, {x, x_ld, w->k, 1}, tokens) || overlap(all, {x_scale, 0, tokens, 4}, 1) || overlap(all, {bias, 0, w->c_out, 4}, 1))
+        return fail(NM_ERR_INVALID_ARG, "%s: y overlaps an input", who);
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return fail(NM_ERR_CUDA, "%s: cudaGetDevice: %s", who, cudaGetErrorString(e));
+    if (dev != w->device) return fail(NM_ERR_INVALID_ARG, "%s: the handle belongs to device %d, current is %d", who, w->device, dev);
+    const Q8Linear p = {w, x, x_ld, x_scale, bias, y, y_ld, tokens, y_dtype, never_loaded};
+    if (never_loaded >= 0) return nmhost::launch_q8_gemm(p, static_cast<cudaStream_t>(cuda_stream));
+    if (nmhost::q8_few_takes(p)) return nmhost::launch_q8_few(p, static_cast<cudaStream_t>(cuda_stream));
+    if (nmhost::q8_pair_takes(p)) return nmhost::launch_q8_pair(p, static_cast<cudaStream_t>(cuda_stream));
+    return nmhost::launch_q8_gemm(p, static_cast<cudaStream_t>(cuda_stream));
+}
+
 extern "C" {
 
 nm_status_t nm_q8_rows(const void* x, long long x_ld, nm_dtype_t dtype, int tokens, int h, int8_t* q, long long q_ld, float* scale,
@@ -499,32 +532,14 @@ nm_status_t nm_q8_weights_free(nm_q8_weights_t* w)
 nm_status_t nm_q8_linear(const nm_q8_weights_t* w, const int8_t* x, long long x_ld, const float* x_scale, int tokens, const float* bias, void* y,
                          long long y_ld, nm_dtype_t y_dtype, void* cuda_stream)
 {
-    if (!valid(w)) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: bad weights handle");
-    if (!known(y_dtype)) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: unknown type");
-    if (tokens < 0) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: tokens must be >= 0");
-    if (tokens > kMostTokens) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: more than 2^30 tokens");
-    if (tokens == 0) return NM_OK;
-    if (!x || !x_scale || !y) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: x, x_scale or y is NULL");
-    if (tokens == 1) {
-        x_ld = (w->k + 15) / 16 * 16;
-        y_ld = w->c_out;
-    }
-    if (x_ld < w->k || y_ld < w->c_out) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: rows are closer than their length");
-    if (x_ld > (1ll << 38)) return fail(NM_ERR_UNSUPPORTED, "nm_q8_linear: rows of x are too far apart");
-    if (at(x) % 16 || x_ld % 16) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: x must be 16-byte aligned with rows a multiple of 16 bytes apart");
-    if (at(y) % size_of(y_dtype) || at(x_scale) % 4 || at(bias) % 4)
-        return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: a tensor is not aligned to its elements");
-    const Span ys = {y, y_ld, w->c_out, size_of(y_dtype)}, all = {y, 0, (tokens - 1) * y_ld + w->c_out, size_of(y_dtype)};
-    if (overlap(ys, {x, x_ld, w->k, 1}, tokens) || overlap(all, {x_scale, 0, tokens, 4}, 1) || overlap(all, {bias, 0, w->c_out, 4}, 1))
-        return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: y overlaps an input");
-    int dev = 0;
-    const cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return fail(NM_ERR_CUDA, "nm_q8_linear: cudaGetDevice: %s", cudaGetErrorString(e));
-    if (dev != w->device) return fail(NM_ERR_INVALID_ARG, "nm_q8_linear: the handle belongs to device %d, current is %d", w->device, dev);
-    const Q8Linear p = {w, x, x_ld, x_scale, bias, y, y_ld, tokens, y_dtype};
-    if (nmhost::q8_few_takes(p)) return nmhost::launch_q8_few(p, static_cast<cudaStream_t>(cuda_stream));
-    if (nmhost::q8_pair_takes(p)) return nmhost::launch_q8_pair(p, static_cast<cudaStream_t>(cuda_stream));
-    return nmhost::launch_q8_gemm(p, static_cast<cudaStream_t>(cuda_stream));
+    return linear("nm_q8_linear", w, x, x_ld, x_scale, tokens, bias, y, y_ld, y_dtype, -1, cuda_stream);
+}
+
+nm_status_t nm_selftest_q8_wait_expiry(const nm_q8_weights_t* w, const int8_t* x, long long x_ld, const float* x_scale, int tokens, float* y,
+                                       long long y_ld, int block, void* cuda_stream)
+{
+    if (block < 0) return fail(NM_ERR_INVALID_ARG, "nm_selftest_q8_wait_expiry: block must be >= 0");
+    return linear("nm_selftest_q8_wait_expiry", w, x, x_ld, x_scale, tokens, nullptr, y, y_ld, NM_F32, block, cuda_stream);
 }
 
 }  // extern "C"

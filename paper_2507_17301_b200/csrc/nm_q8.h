@@ -58,6 +58,7 @@ struct Q8Linear {
     long long y_ld;
     int tokens;
     nm_dtype_t y_type;
+    int never_loaded;      // nm_q8_gemm.cu: block of columns from which on nothing is loaded (self-test), -1: none
 };
 
 namespace nmhost {

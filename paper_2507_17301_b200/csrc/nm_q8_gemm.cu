@@ -46,6 +46,7 @@ struct GemmArgs {
     int ks;       // CTAs of a cluster = ranges of the reduction axis
     int stages, stage_bytes;
     int tmem;     // columns of tensor memory
+    int never_loaded;   // block from which on nothing is loaded, so that the wait for it expires (self-test); -1: none
 };
 
 template <typename T>
@@ -129,7 +130,8 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
             RingPos rp;
             int issued = 0;
             bool after = false;   // the kernel before has ended
-            for (int kb = kb0; kb < kb1; ++kb) {
+            const int end = g.never_loaded >= kb0 && g.never_loaded < kb1 ? g.never_loaded : kb1;
+            for (int kb = kb0; kb < end; ++kb) {
                 if (rp.wrapped && !mbar_wait_lone(smem_u32(&s_free[rp.s]), rp.parity ^ 1u)) { *abort_flag = 1; break; }
                 const uint32_t at = ring + rp.s * g.stage_bytes, bar = smem_u32(&s_full[rp.s]);
                 mbar_arrive_expect_tx(bar, static_cast<uint32_t>(g.stage_bytes));
@@ -151,6 +153,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
                 ++issued;
             }
             if (!after) pdl_wait();
+            (void)mbar_wait(smem_u32(&s_acc), 0);   // the issuer is through with the stages, or has given up and said so
             if (*abort_flag != 0) {
                 // let the loads in flight land
                 for (int back = 0; back < g.stages && back < issued; ++back) {
@@ -164,7 +167,9 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
         if (elect_one()) {
             const uint32_t idesc = umma_idesc_s8(128, g.bn) | (SPARSE ? kSparseA : 0u);
             RingPos rp;
-            for (int kb = kb0; kb < kb1; ++kb) {
+            pdl_wait();   // (its waits are bounded: the time that the kernel before still takes is no part of them)
+            int kb = kb0;
+            for (; kb < kb1; ++kb) {
                 if (!mbar_wait_lone(smem_u32(&s_full[rp.s]), rp.parity)) { *abort_flag = 2; break; }
                 tc_fence_after();
                 const uint32_t at = ring + rp.s * g.stage_bytes;
@@ -185,6 +190,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
                 umma_commit(smem_u32(&s_free[rp.s]));
                 rp.advance(g.stages);
             }
+            if (kb < kb1) __threadfence_block();   // the flag is seen by whoever sees the commit, which waits for the MMAs issued so far
             umma_commit(smem_u32(&s_acc));
         }
     } else {
@@ -202,6 +208,7 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
         const bool aligned = g.y_ld % 4 == 0 && reinterpret_cast<uintptr_t>(g.y) % (4 * sizeof(T)) == 0;
         const bool ok = mbar_wait(smem_u32(&s_acc), 0);
         if (!ok) *abort_flag = 3;
+        const int given_up = *abort_flag;   // the issuer: its sums are written nowhere (asked below, so that nobody waits for the load)
         tc_fence_after();
         // sums by token into the ring, whose loads have all been used: a lane holds a channel of 32 tokens, a row of the ring is a token
         const uint32_t mine = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
@@ -215,12 +222,12 @@ __global__ void __launch_bounds__(THREADS, 2) k_q8_gemm(const GemmArgs g, const 
         }
         const int run = g.bn / g.ks;   // tokens that this CTA finishes
         uint32_t parts = ring;
-        bool complete = ok;
+        bool complete = ok && given_up == 0;
         if (g.ks > 1) {
-            // each CTA's run of tokens to that CTA
+            // each CTA's run of tokens to that CTA (one that has given up sends nothing, and the waits of all of them expire)
             fence_proxy_async();
             asm volatile("bar.sync 1, 128;" ::: "memory");
-            if (e == 0) {
+            if (e == 0 && complete) {
                 for (int d = 0; d < g.ks; ++d)
                     bulk_copy_cluster(mapa_shared(recv + rank * run * 512u, d), ring + static_cast<uint32_t>(d * run) * 512u, static_cast<uint32_t>(run) * 512u,
                                       mapa_shared(smem_u32(&s_recv), d));
@@ -293,6 +300,7 @@ nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
     g.weights = sparse ? w->sparse : w->expanded; g.places = w->places; g.w_scale = w->scales; g.x_scale = p.x_scale; g.bias = p.bias; g.y = p.y; g.y_ld = p.y_ld; g.status = w->status;
     g.tokens = p.tokens; g.c_out = w->c_out; g.rows = w->rows;
     g.blocks = sparse ? w->s_blocks : w->k_blocks;
+    g.never_loaded = p.never_loaded;
     g.c_tiles = (w->c_out + 127) / 128;
     // The narrowest tiles (in sixteens) that still are one round, us: 4096 -> 4096, 128 tokens in tiles of 16 / 32 / 64 / 128: 16.0 / 8.7 / 9.2 /
     // 11.1; 512 tokens: 56 / 34 / 19 / 12.2.  A split of the reduction axis pays where half the SMs would idle (16 tokens, 2048 -> 2048: 5.0

@@ -98,6 +98,8 @@ def _load():
     lib.nm_q8_weights_check.argtypes = [vp, vp]
     lib.nm_q8_weights_free.argtypes = [vp]
     lib.nm_q8_linear.argtypes = [vp, vp, ll, vp, i, vp, vp, ll, i, vp]
+    lib.nm_selftest_q8_wait_expiry.argtypes = [vp, vp, ll, vp, i, vp, ll, i, vp]
+    lib.nm_selftest_q8_wait_expiry.restype = ctypes.c_int
     for name in ("rows", "silu_mul", "rmsnorm", "prune", "weights_import", "weights_export", "weights_dims", "weights_check",
                  "weights_free", "linear"):
         getattr(lib, "nm_q8_" + name).restype = ctypes.c_int
@@ -124,7 +126,7 @@ _nm_binding.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
 EXPORTS = ("nm_memory_trim", "nm_plan_key", "nm_plan_cache_store", "nm_plan_cache_lookup", "nm_selftest_wait_expiry", "nm_maxpool2d", "nm_weights_retained_l1", "nm_conv2d_res", "nm_plan_scratch_bytes", "nm_weights_reserve", "nm_prune", "nm_prune_noalloc", "nm_weights_dims", "nm_weights_export", "nm_weights_import", "nm_weights_check",
            "nm_weights_free", "nm_conv2d", "nm_conv2d_host", "nm_autotune", "nm_autotune_tile",
            "nm_q8_rows", "nm_q8_silu_mul", "nm_q8_rmsnorm", "nm_q8_prune", "nm_q8_weights_import", "nm_q8_weights_export",
-           "nm_q8_weights_dims", "nm_q8_weights_check", "nm_q8_weights_free", "nm_q8_linear",
+           "nm_q8_weights_dims", "nm_q8_weights_check", "nm_q8_weights_free", "nm_q8_linear", "nm_selftest_q8_wait_expiry",
            "nm_status_string", "nm_last_error", "nm_launch_count")
 
 
@@ -492,3 +494,16 @@ def nm_q8_linear(w: Q8Weights, xq: torch.Tensor, x_scale: torch.Tensor, bias: to
                  out_dtype: torch.dtype = torch.bfloat16, y: torch.Tensor | None = None) -> torch.Tensor:
     """Product of 8-bit rows ``xq [tokens, k]`` with the layer's weights: ``[tokens, c_out]`` in ``out_dtype`` (or ``y``'s type)."""
     return _q8_out(_nm_binding.q8_linear(w._addr, w.c_out, w.k, xq, x_scale, bias, out_dtype, y))
+
+
+def nm_selftest_q8_wait_expiry(w: Q8Weights, xq: torch.Tensor, x_scale: torch.Tensor, y: torch.Tensor, block: int = 0):
+    """The product into ``y`` (fp32 ``[tokens, c_out]``), of which block ``block`` of the columns is never loaded: its wait expires, ``y`` stays
+    as it was, and ``nm_q8_weights_check`` reports it."""
+    if not (xq.is_cuda and xq.dtype == torch.int8 and xq.dim() == 2 and xq.shape[1] == w.k and xq.stride(1) == 1
+            and xq.device == w.device == y.device and y.dtype == torch.float32 and tuple(y.shape) == (xq.shape[0], w.c_out) and y.stride(1) == 1):
+        raise TypeError("xq must be int8 [tokens, k] and y float32 [tokens, c_out], both CUDA tensors with contiguous rows")
+    if _dev_f32(x_scale, "x_scale") and x_scale.numel() != xq.shape[0]:
+        raise TypeError("x_scale must have one element for each token")
+    with torch.cuda.device(w.device):
+        _check(_lib.nm_selftest_q8_wait_expiry(w.handle, xq.data_ptr(), xq.stride(0), x_scale.data_ptr(), xq.shape[0], y.data_ptr(),
+                                               y.stride(0), block, _stream()))

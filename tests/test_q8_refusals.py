@@ -118,3 +118,11 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
         nm.nm_q8_prune(x, 2, 4, 8)
     with pytest.raises(TypeError, match="values"):
         nm.nm_q8_weights_import(x.to(torch.int8), x[:, 0].contiguous(), x.to(torch.uint16), 64, 2, 4, 4)
+
+
+def test_the_self_test_refuses_what_the_product_refuses():
+    w = _Fake()
+    call = lambda h=w.addr, x=X, x_ld=96, xs=SC, tokens=3, y=S, y_ld=128, block=0: nm._lib.nm_selftest_q8_wait_expiry(h, x, x_ld, xs, tokens, y, y_ld, block, None)  # noqa: E731
+    for bad in ({"h": None}, {"block": -1}, {"x": None}, {"xs": None}, {"y": None}, {"tokens": -2}, {"x_ld": 80}, {"x": X + 8}, {"y_ld": 127}, {"y": X + 64}):
+        assert call(**bad) == nm.NM_ERR_INVALID_ARG, bad
+    assert call(tokens=0) == nm.NM_OK
