@@ -7,6 +7,7 @@
 // nm.py has loaded (NM_LIBRARY included) is the one that runs.
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -292,12 +293,21 @@ bool dtype_of(at::ScalarType t, nm_dtype_t* out)
     return true;
 }
 
+// Whether a call under autograd would have to differentiate with respect to `t`, which no 8-bit operator does; sets a TypeError.
+bool wants_gradient(const at::Tensor& t, const char* what)
+{
+    if (!at::GradMode::is_enabled() || !t.requires_grad()) return false;
+    PyErr_Format(PyExc_TypeError, "%s requires gradients, which the 8-bit operators do not give (call them under torch.no_grad())", what);
+    return true;
+}
+
 // A tensor [rows][cols] whose rows are contiguous, or NULL with a TypeError set; rows and cols of -1: any.
 const at::Tensor* matrix(PyObject* obj, const char* what, const char* type_name, bool type_ok(at::ScalarType), int64_t rows, int64_t cols,
                          const at::Tensor* beside)
 {
     if (THPVariable_Check(obj)) {
         const at::Tensor& t = THPVariable_Unpack(obj);
+        if (wants_gradient(t, what)) return nullptr;
         if (t.is_cuda() && t.layout() == at::kStrided && type_ok(t.scalar_type()) && t.dim() == 2 && (t.size(1) < 2 || t.stride(1) == 1)) {
             if ((rows >= 0 && t.size(0) != rows) || (cols >= 0 && t.size(1) != cols)) {
                 PyErr_Format(PyExc_TypeError, "%s must be [%lld, %lld] (got [%lld, %lld])", what, static_cast<long long>(rows >= 0 ? rows : t.size(0)),
@@ -323,6 +333,7 @@ const at::Tensor* vector(PyObject* obj, const char* what, const char* type_name,
 {
     if (THPVariable_Check(obj)) {
         const at::Tensor& t = THPVariable_Unpack(obj);
+        if (wants_gradient(t, what)) return nullptr;
         if (t.is_cuda() && t.layout() == at::kStrided && type_ok(t.scalar_type()) && t.dim() == 1 && t.is_contiguous() && t.size(0) == n &&
             t.device() == beside.device())
             return &t;

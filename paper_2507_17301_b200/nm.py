@@ -386,6 +386,8 @@ def nm_autotune_tile(w_dense: torch.Tensor, n_keep: int, m_group: int, tile_cand
 
 
 # ---- linear layers of language models in 8 bits -------------------------------------------------------------------
+# Inference only: nm_q8_rows, nm_q8_silu_mul, nm_q8_rmsnorm and nm_q8_linear refuse a tensor that requires gradients (TypeError) unless
+# gradients are off (torch.no_grad(), torch.inference_mode()), for their outputs would carry none.
 
 
 class Q8Weights:
