@@ -127,10 +127,35 @@ __global__ void __launch_bounds__(256) k_q8_indices(const uint16_t* __restrict__
     }
 }
 
-// Expanded form from the handle's indices and values [c_out][kk]: a block writes 64 rows of a 128-column block.  (Index rows out of
-// order give a wrong place, never one outside a row.)
+// 32 columns of a row in the sparse form: 16 bytes and a word of places.  Of four columns the two that are not zero, or as many as there
+// are and the first others.
+__device__ __forceinline__ void store_sparse(const nm_q8_weights& h, int kb, int r, int quarter, const uint32_t (&in)[8])
+{
+    uint32_t out[4] = {0u, 0u, 0u, 0u}, places = 0u;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        uint32_t set = 0u;   // columns that are not zero
+        for (int b = 0; b < 4; ++b)
+            if (in[q] >> (8 * b) & 0xFFu) set |= 1u << b;
+        for (int b = 0; b < 4 && __popc(set) < 2; ++b) set |= 1u << b;
+        const int first = __ffs(set) - 1, second = __ffs(set & (set - 1u)) - 1;
+        places |= static_cast<uint32_t>(first | second << 2) << (4 * q);
+        const uint32_t two = (in[q] >> (8 * first) & 0xFFu) | (in[q] >> (8 * second) & 0xFFu) << 8;
+        out[q / 2] |= two << (16 * (q % 2));
+    }
+    const int sb = kb / 2, eighth = kb % 2 * 4 + quarter;
+    uint8_t* dst = reinterpret_cast<uint8_t*>(h.sparse) + (static_cast<size_t>(sb) * h.rows + r) * 128;
+    *reinterpret_cast<uint4*>(dst + ((eighth ^ (r & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
+    uint8_t* to = h.places + (static_cast<size_t>(sb) * (h.rows / 128) + r / 128) * 4096;
+    *reinterpret_cast<uint32_t*>(to + r % 128 / 8 * 256 + eighth / 4 * 128 + r % 8 * 16 + eighth % 4 * 4) = places;
+}
+
+// The form that the tensor core reads, sparse or expanded, from the handle's indices and values [c_out][kk]: a block writes 64 rows of
+// 128 columns, a thread 16 bytes of a row.  (Index rows out of order give a wrong place, never one outside a row.)
+template <bool SPARSE>
 __global__ void __launch_bounds__(256) k_q8_expand(const int8_t* __restrict__ values, const nm_q8_weights h)
 {
+    constexpr int COLS = SPARSE ? 32 : 16, PIECES = 128 / COLS;
     __shared__ int s_pos[128];   // place of a column among the tile's retained ones, -1: pruned
     const int kb = blockIdx.x, row0 = blockIdx.y * 64;
     for (int r0 = row0; r0 < row0 + 64 && r0 < h.rows;) {
@@ -154,54 +179,25 @@ __global__ void __launch_bounds__(256) k_q8_expand(const int8_t* __restrict__ va
             s_pos[threadIdx.x] = pos;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < (r1 - r0) * 8; i += 256) {
-            const int r = r0 + i / 8, piece = i % 8;
-            uint32_t word[4] = {0u, 0u, 0u, 0u};
+        for (int i = threadIdx.x; i < (r1 - r0) * PIECES; i += 256) {
+            const int r = r0 + i / PIECES, piece = i % PIECES;
+            uint32_t word[COLS / 4] = {};
             if (r < h.c_out) {
 #pragma unroll
-                for (int b = 0; b < 16; ++b) {
-                    const int pos = s_pos[piece * 16 + b];
+                for (int b = 0; b < COLS; ++b) {
+                    const int pos = s_pos[piece * COLS + b];
                     if (pos >= 0) word[b / 4] |= (static_cast<uint32_t>(values[static_cast<size_t>(r) * h.kk + pos]) & 0xFFu) << (8 * (b % 4));
                 }
             }
-            uint8_t* dst = reinterpret_cast<uint8_t*>(h.expanded) + (static_cast<size_t>(kb) * h.rows + r) * 128 + ((piece ^ (r & 7)) << 4);
-            *reinterpret_cast<uint4*>(dst) = make_uint4(word[0], word[1], word[2], word[3]);
+            if constexpr (SPARSE) {
+                store_sparse(h, kb, r, piece, word);
+            } else {
+                uint8_t* dst = reinterpret_cast<uint8_t*>(h.expanded) + (static_cast<size_t>(kb) * h.rows + r) * 128 + ((piece ^ (r & 7)) << 4);
+                *reinterpret_cast<uint4*>(dst) = make_uint4(word[0], word[1], word[2], word[3]);
+            }
         }
         r0 = r1;
     }
-}
-
-// Sparse form out of the expanded one: a thread takes 32 columns of a row, 16 bytes and a word of places.  Of four columns the two
-// that are not zero, or as many as there are and the first others.
-__global__ void __launch_bounds__(256) k_q8_sparse(const nm_q8_weights h)
-{
-    const int i = blockIdx.x * 256 + threadIdx.x, r = i / 8, eighth = i % 8, sb = blockIdx.y;
-    if (r >= h.rows) return;
-    uint32_t in[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u}, out[4] = {0u, 0u, 0u, 0u}, places = 0u;
-    const int kb = sb * 2 + eighth / 4;
-    if (kb < h.k_blocks) {
-        const uint8_t* row = reinterpret_cast<const uint8_t*>(h.expanded) + (static_cast<size_t>(kb) * h.rows + r) * 128;
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const uint4 u = *reinterpret_cast<const uint4*>(row + (((eighth % 4 * 2 + p) ^ (r & 7)) << 4));
-            in[p * 4] = u.x; in[p * 4 + 1] = u.y; in[p * 4 + 2] = u.z; in[p * 4 + 3] = u.w;
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        uint32_t set = 0u;   // columns that are not zero
-        for (int b = 0; b < 4; ++b)
-            if (in[q] >> (8 * b) & 0xFFu) set |= 1u << b;
-        for (int b = 0; b < 4 && __popc(set) < 2; ++b) set |= 1u << b;
-        const int first = __ffs(set) - 1, second = __ffs(set & (set - 1u)) - 1;
-        places |= static_cast<uint32_t>(first | second << 2) << (4 * q);
-        const uint32_t two = (in[q] >> (8 * first) & 0xFFu) | (in[q] >> (8 * second) & 0xFFu) << 8;
-        out[q / 2] |= two << (16 * (q % 2));
-    }
-    uint8_t* dst = reinterpret_cast<uint8_t*>(h.sparse) + (static_cast<size_t>(sb) * h.rows + r) * 128;
-    *reinterpret_cast<uint4*>(dst + ((eighth ^ (r & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
-    uint8_t* to = h.places + (static_cast<size_t>(sb) * (h.rows / 128) + r / 128) * 4096;
-    *reinterpret_cast<uint32_t*>(to + r % 128 / 8 * 256 + eighth / 4 * 128 + r % 8 * 16 + eighth % 4 * 4) = places;
 }
 
 // Most columns that an N:M pattern can keep of four aligned ones of k.
@@ -240,14 +236,25 @@ __global__ void __launch_bounds__(256) k_q8_pack(const int8_t* __restrict__ valu
     }
 }
 
-// values [c_out][kk] out of the expanded form.
+// values [c_out][kk] out of the sparse or the expanded form.
 __global__ void __launch_bounds__(256) k_q8_values(const nm_q8_weights h, int8_t* __restrict__ values)
 {
     const int j = blockIdx.x * 256 + threadIdx.x;
     if (j >= h.kk) return;
     for (int o = blockIdx.y; o < h.c_out; o += gridDim.y) {
-        const int c = h.indices[static_cast<size_t>(o / h.tile_t) * h.kk_ld + j], piece = c % 128 / 16;
-        values[static_cast<size_t>(o) * h.kk + j] = h.expanded[(static_cast<size_t>(c / 128) * h.rows + o) * 128 + ((piece ^ (o & 7)) << 4) + c % 16];
+        const int c = h.indices[static_cast<size_t>(o / h.tile_t) * h.kk_ld + j];
+        int8_t value;
+        if (h.sparse) {   // (see store_sparse; a column that is in neither place is a zero)
+            const int sb = c / 256, eighth = c % 256 / 32, four = c % 32 / 4;
+            const uint8_t* from = h.places + (static_cast<size_t>(sb) * (h.rows / 128) + o / 128) * 4096;
+            const uint32_t two = *reinterpret_cast<const uint32_t*>(from + o % 128 / 8 * 256 + eighth / 4 * 128 + o % 8 * 16 + eighth % 4 * 4) >> (4 * four);
+            const int8_t* at = h.sparse + (static_cast<size_t>(sb) * h.rows + o) * 128 + ((eighth ^ (o & 7)) << 4) + 2 * four;
+            value = (two & 3u) == c % 4u ? at[0] : (two >> 2 & 3u) == c % 4u ? at[1] : static_cast<int8_t>(0);
+        } else {
+            const int piece = c % 128 / 16;
+            value = h.expanded[(static_cast<size_t>(c / 128) * h.rows + o) * 128 + ((piece ^ (o & 7)) << 4) + c % 16];
+        }
+        values[static_cast<size_t>(o) * h.kk + j] = value;
     }
 }
 
@@ -282,7 +289,7 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
         total += (bytes + 1023) / 1024 * 1024;
         return here;
     };
-    const size_t at_expanded = place(static_cast<size_t>(h->k_blocks) * h->rows * 128);
+    const size_t at_expanded = place(h->s_blocks ? 0 : static_cast<size_t>(h->k_blocks) * h->rows * 128);
     const size_t tiles = n_keep == m_group ? 1 : h->n_tiles;
     const size_t at_packed = place(tiles * h->units * 8 * h->kk_ld);
     const size_t at_sparse = place(static_cast<size_t>(h->s_blocks) * h->rows * 128), at_places = place(static_cast<size_t>(h->s_blocks) * h->rows * 32);
@@ -294,7 +301,7 @@ nm_status_t make(const char* who, int c_out, int k, int n_keep, int m_group, int
         delete h;
         return fail(NM_ERR_ALLOC, "%s: cannot allocate %zu bytes on the device", who, total);
     }
-    h->expanded = reinterpret_cast<int8_t*>(h->block + at_expanded);
+    if (!h->s_blocks) h->expanded = reinterpret_cast<int8_t*>(h->block + at_expanded);
     h->packed = h->units ? reinterpret_cast<int8_t*>(h->block + at_packed) : nullptr;
     h->indices = reinterpret_cast<uint16_t*>(h->block + at_indices);
     if (h->s_blocks) {
@@ -321,15 +328,12 @@ nm_status_t finish(const char* who, nm_q8_weights* h, const int8_t* values, cons
     cudaError_t e = cudaMemsetAsync(h->status, 0, 16, st);
     int* bad = h->status + 3;
     if (idx) k_q8_indices<<<dim3((h->kk_ld + 255) / 256, h->n_tiles), 256, 0, st>>>(idx, *h, bad);
-    k_q8_expand<<<dim3(h->k_blocks, h->rows / 64), 256, 0, st>>>(values, *h);
+    if (h->sparse) k_q8_expand<true><<<dim3(2 * h->s_blocks, h->rows / 64), 256, 0, st>>>(values, *h);
+    else k_q8_expand<false><<<dim3(h->k_blocks, h->rows / 64), 256, 0, st>>>(values, *h);
     nmhost::count_launch(idx ? 2 : 1);
     if (h->packed) {
         const int tile = packed_tile(*h), n_units = (h->c_out + tile - 1) / tile * h->units;
         k_q8_pack<<<dim3((h->kk_ld / 64 + 7) / 8, std::min(n_units, 65535)), 256, 0, st>>>(values, *h, tile);
-        nmhost::count_launch(1);
-    }
-    if (h->sparse) {
-        k_q8_sparse<<<dim3(h->rows / 32, h->s_blocks), 256, 0, st>>>(*h);
         nmhost::count_launch(1);
     }
     if (e == cudaSuccess) e = cudaGetLastError();
@@ -479,7 +483,7 @@ nm_status_t nm_q8_weights_export(const nm_q8_weights_t* w, int8_t* values, float
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = cudaSuccess;
     if (values) {
-        if (!nmhost::kernel_may_touch(values, w->expanded, w->device))
+        if (!nmhost::kernel_may_touch(values, w->scales, w->device))
             return fail(NM_ERR_INVALID_ARG, "nm_q8_weights_export: values must lie on the handle's device, which is the current one");
         k_q8_values<<<dim3((w->kk + 255) / 256, std::min(w->c_out, 65535)), 256, 0, st>>>(*w, values);
         nmhost::count_launch(1);

@@ -23,7 +23,8 @@ struct nm_q8_weights {
     int8_t* packed;        // [tile][unit][kk_ld / 64][8 rows x 4 quarters][16]: retained weights, zeros behind the last column and row; the 512
                            // bytes of a unit and 64 columns are one warp's load, row and quarter by lane.  NULL for tiles of less than 8 rows
     int8_t* expanded;      // [k_blocks][rows][128]: pruned columns are zeros; a row's eight 16-byte pieces stand in the order of the
-                           // tensor core's 128-byte swizzle (piece i of row r at i ^ (r & 7))
+                           // tensor core's 128-byte swizzle (piece i of row r at i ^ (r & 7)).  NULL where there is a sparse form, which every
+                           // product reads instead (4096 -> 12288 at 2:4: 1.2 bytes a dense weight in all, 2.2 with both)
     int8_t* sparse;        // [s_blocks][rows][128]: two of every four columns, the others are zeros; pieces as in `expanded`
     uint8_t* places;       // [s_blocks][rows / 128][4096]: which two, four bits for four columns, 32 bytes a row, as the image that
                            // tmem_cp_128x256b reads: 8-row groups of two 128-byte halves, 16 bytes of each row in a half
