@@ -91,7 +91,7 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity)
         : "memory");
     return ok != 0;
 }
-// Bounded wait: about a second at worst, then gives up and reports false.
+// Bounded wait, then gives up and reports false: after half a second for a thread alone, up to 17 where all threads of a cluster's CTAs wait.
 constexpr uint32_t kWaitPolls = 1u << 22;
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity)
 {

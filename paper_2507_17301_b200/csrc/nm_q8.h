@@ -68,7 +68,7 @@ nm_status_t launch_q8_rows_f32(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_ty
 nm_status_t launch_q8_rows_bf16(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
 nm_status_t launch_q8_rows_f16(Q8RowOp op, const Q8Rows& a, nm_dtype_t weight_type, bool vec, cudaStream_t st);
 
-// nm_q8_few.cu: few tokens (32 at most); false where the kernel does not take the call
+// nm_q8_few.cu: few tokens (8 at most, 4 of a dense layer or one of narrow tiles); false where the kernel does not take the call
 bool q8_few_takes(const Q8Linear& p);
 nm_status_t launch_q8_few(const Q8Linear& p, cudaStream_t st);
 

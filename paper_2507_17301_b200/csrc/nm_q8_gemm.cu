@@ -29,6 +29,11 @@ constexpr int NSTAGE_MAX = 8;
 constexpr int A_BYTES = 128 * 128;
 constexpr int MOST_TOKENS = 128;   // of a tile; more than a round of such tiles is the pair kernel's
 constexpr int PLACES = 4096;   // bytes of a sparse stage's places
+constexpr int RING_ALONE = 224 * 1024 - 1024 - 2048, RING_SHARED = 112 * 1024 - 1024 - 2048;   // bytes for a CTA's ring, alone on its SM and beside another
+// A tile's sums go through the ring, 512 bytes a token.  Two stages hold them, at any width, and every ring has two (a stage of sparse
+// weights is the longer one; a cluster's CTA alone on its SM also holds the sums it receives).
+static_assert(2 * (A_BYTES + MOST_TOKENS * 128) >= MOST_TOKENS * 512, "two stages hold a tile's sums");
+static_assert(2 * (A_BYTES + PLACES + 2 * MOST_TOKENS * 128) <= RING_SHARED && RING_SHARED <= RING_ALONE - MOST_TOKENS * 512, "two stages fit");
 
 struct GemmArgs {
     const int8_t* weights;     // expanded or sparse
@@ -315,9 +320,8 @@ nm_status_t launch_q8_gemm(const Q8Linear& p, cudaStream_t st)
     // 4096 -> 4096, 512 tokens 12.2 us against 16.9)
     const bool half = items > sm_count();
     g.stage_bytes = sparse ? A_BYTES + PLACES + 2 * g.bn * 128 : A_BYTES + g.bn * 128;
-    const int budget = (half ? 112 : 224) * 1024 - 1024 - 2048 - (g.ks > 1 ? g.bn * 512 : 0);
+    const int budget = (half ? RING_SHARED : RING_ALONE) - (g.ks > 1 ? g.bn * 512 : 0);
     g.stages = std::min(NSTAGE_MAX, budget / g.stage_bytes);
-    // (the sums of a tile, bn * 512 bytes, at most 64 KB, go through the ring, which has at least 96 KB)
     g.tmem = 32;
     while (g.tmem < g.bn + (sparse ? 8 * g.stages : 0)) g.tmem *= 2;
     alignas(64) CUtensorMap tm;

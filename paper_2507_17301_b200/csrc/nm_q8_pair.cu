@@ -9,18 +9,19 @@
 // memory, two tiles of 256 columns in turn, so that one is written out while the next is added up.
 // In the sparse form (patterns that keep at most two of four aligned columns) a stage is 256 columns, 16 KB of weights, 4 KB of their places,
 // which go to tensor memory ahead of the MMAs, and 28 KB of activations: 224 tokens a tile, so that the places of four stages fit beside
-// the sums.  4096 -> 12288 at 2:4, 8192 tokens: 242 us expanded, 184 sparse (2.2 POP/s on the retained weights).  A stage takes 690 cycles,
-// not the 448 of the sparse rate: without the loads of activations it still takes 605 (480 with 128 tokens a tile, 570 with 192: about
-// 75 cycles an instruction whatever its width), and the copy of the places is no more than 10 of them.  Stages of the expanded form take
-// 520 of 512.
+// the sums.  4096 -> 12288 at 2:4, 8192 tokens: 242 us expanded, 183 sparse (2.2 POP/s on the retained weights) at 1.65 GHz or more; in a
+// run of a second or longer the power limit takes the clock to 1.3 GHz and a call to 218.  A stage takes 690 cycles, not the 448 of the
+// sparse rate: without the loads of activations it still takes 605 (480 with 128 tokens a tile, 570 with 192: an instruction of 128, 192
+// and 224 tokens 120, 142 and 151 cycles, where its rate is 64, 96 and 112), and the copy of the places is no more than 10 of them.  What
+// the rest is has not been found.  Stages of the expanded form take 520 of 512.
 //
 //   producer (1 thread per CTA)   a bulk copy of the weights' swizzled image and a TMA load of the activations per stage
 //   relay (1 thread, second CTA)  forwards "stage landed" to the first CTA's barrier
 //   MMA issuer (1 thread, first CTA)
 //   epilogue (8 warps per CTA)    a lane has a channel of 16 tokens: y = (sum * x_scale) * w_scale + bias, transposed through shared
 //                                 memory to rows of 32 channels
-// A work item is 256 channels x 256 tokens, items of one token block follow one another; pairs walk them in a static persistent
-// schedule.  Every wait is bounded; the two cluster-wide barriers at start and end are reached by all threads unconditionally.
+// A work item is 256 channels x 256 tokens (224 in the sparse form), items of one token block follow one another; pairs walk them in a
+// static persistent schedule.  Every wait is bounded; the two cluster-wide barriers at start and end are reached by all threads unconditionally.
 #include <atomic>
 
 #include <cuda_bf16.h>
